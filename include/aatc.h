@@ -456,6 +456,176 @@ aatc_status_t aatc_bf16_decode_attention(const void* K, const void* V, const voi
                                          int32_t n_kv_heads, int32_t n_q_heads, float* out,
                                          void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Paged cache of uncompressed keys and values.  New tokens of a batch of sequences of different
+ * lengths are kept as they are, in pages that any sequence can own or share; tokens that have
+ * become old go on to the packed cache (aatc_paged_gather, aatc_encode), and one softmax covers
+ * both (aatc_decode_attention_lse gives the packed part, which aatc_paged_decode_attention
+ * joins as its prior).  The paper has no counterpart: it keeps a recent window in full precision
+ * (Sec. 6 setup) and leaves its storage open.
+ *
+ * Pages of one layer: [n_pages][keys | values][n_kv_heads][page_size][128], so a page is one
+ * contiguous block and the tokens of one kv-head in it are one contiguous run.  A sequence is a
+ * row of a block table (device int32 [rows][max_pages], rows table_stride entries apart): its
+ * token i is at offset i % page_size of page table[row][i / page_size].  The ids in a table are
+ * read on the device, so the library cannot refuse a bad one before the launch: every kernel
+ * checks each id and length that it reads, skips what lies outside the pool, and raises a bit of
+ * the caller's flags (dev_flags: device int32, ORed into, may be NULL):
+ *   bit 2 (4): a page id outside [0, n_pages);  bit 3 (8): a row, index or length outside the table.
+ * Base pointers are 16-byte aligned, and strides (in elements) of keys, values and queries are
+ * multiples of 8; the 128 values of one head are contiguous.
+ */
+typedef enum { AATC_BF16 = 0, AATC_F16 = 1 } aatc_dtype_t;
+
+typedef struct {
+  int32_t dtype;        /* aatc_dtype_t of keys, values and queries */
+  int32_t n_kv_heads;   /* 1 .. 4096 */
+  int32_t page_size;    /* tokens per page: 8, 16, 32, 64, 128 or 256 */
+  int32_t n_pages;      /* 1 .. 2^24, with at most 2^40 bytes per layer */
+} aatc_pages_t;
+
+/* Bytes of one layer's pages.  Errors: AATC_ERR_INVALID_ARG. */
+aatc_status_t aatc_pages_bytes(const aatc_pages_t* pages, size_t* bytes);
+
+/*
+ * Rotary positions.  The first rot_dim dimensions of a head are rot_dim / 2 pairs: (i, i + rot_dim / 2)
+ * in the half layout, (2 i, 2 i + 1) in the interleaved one; the others are left as they are.  The pair i
+ * of a token at position p, (a, b), becomes factor * (a cos t - b sin t, a sin t + b cos t), t = p w_i.
+ *
+ * aatc_rotary_frequencies (host only): w_i = base^(-2 i / rot_dim) scaled for long contexts:
+ *   AATC_ROPE_PLAIN   as it is
+ *   AATC_ROPE_LINEAR  w_i / s
+ *   AATC_ROPE_NTK     base replaced by base s^(rot_dim / (rot_dim - 2)): the slowest pair is slowed by s
+ *   AATC_ROPE_RAMP    with e(n) = rot_dim ln(original / (2 pi n)) / (2 ln base), the pair index that
+ *                     turns n times over the original context, lo = max(0, floor e(p0)),
+ *                     hi = min(rot_dim - 1, ceil e(p1)), t = clamp((i - lo) / max(hi - lo, 0.001), 0, 1):
+ *                     w_i (t / s + 1 - t), and factor = 0.1 ln s + 1 (s > 1)
+ *   AATC_ROPE_BANDED  with u = clamp((original w_i / (2 pi) - p0) / (p1 - p0), 0, 1): w_i (u + (1 - u) / s)
+ *   s : scale >= 1;  p0, p1 : turns (ramp: fast, slow; banded: low, high), not read by the others
+ *   freq_out : host fp64 [rot_dim / 2];  factor_out : host fp64
+ * aatc_rotary_turns (host only): a frequency as a 64-bit binary fraction of a turn, w / (2 pi) mod 1,
+ * rounded.  The kernels multiply it by the position in integers, which is the angle modulo one turn
+ * without rounding, however long the context.
+ * Errors: AATC_ERR_INVALID_ARG (null; rot_dim not a multiple of 16 in 16 .. 128; base <= 1, s < 1 or a
+ * non-finite value; original < 1; ramp: p0 < p1 or p1 <= 0; banded: p1 <= p0; unknown scaling).
+ */
+typedef enum {
+  AATC_ROPE_PLAIN = 0, AATC_ROPE_LINEAR = 1, AATC_ROPE_NTK = 2, AATC_ROPE_RAMP = 3, AATC_ROPE_BANDED = 4
+} aatc_rope_scaling_t;
+aatc_status_t aatc_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double scale, int32_t original,
+                                      double p0, double p1, double* freq_out, double* factor_out);
+aatc_status_t aatc_rotary_turns(const double* freq, int32_t n, uint64_t* turns_out);
+
+typedef struct {
+  const uint64_t* turns;  /* device [rot_dim / 2], from aatc_rotary_turns */
+  int32_t rot_dim;        /* multiple of 16, 16 .. 128 */
+  int32_t interleaved;    /* 0: half layout, 1: interleaved */
+  float factor;           /* finite */
+} aatc_rotary_t;
+
+/*
+ * Rotate x [n_tokens][n_heads][128] by the tokens' positions.  backward != 0 turns the other way (with the
+ * same factor): the gradient with respect to x, given the gradient of out.  fp32 arithmetic, one rounding.
+ *   positions : device int32 [n_tokens], of any sign
+ *   x, out    : device, token and head strides in elements; out may be x itself (same strides), and
+ *               must not overlap it otherwise
+ * Errors: AATC_ERR_INVALID_ARG.  n_tokens == 0 is a no-op.
+ */
+aatc_status_t aatc_rotate(const aatc_rotary_t* rope, int32_t dtype, const void* x, int64_t x_token_stride,
+                          int64_t x_head_stride, const int32_t* positions, int32_t n_tokens, int32_t n_heads,
+                          int32_t backward, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                          void* stream);
+
+/*
+ * Append: write the keys and values of n_tokens new tokens to their places in the pages, the keys rotated by
+ * the tokens' positions, and rotate the tokens' queries, in one launch.
+ *   rows      : device int32 [n_tokens], the table row of each token, or NULL: token t belongs to row t
+ *   index     : device int32 [n_tokens], the token's index in its sequence; negative: nothing is
+ *               written to the pages for it (padding).  Two tokens of one call with the same place are
+ *               the caller's error: one of them, or parts of both, will be there.
+ *   positions : device int32 [n_tokens] for the rotation, or NULL: the index
+ *   k, v      : device [n_tokens][n_kv_heads][128]
+ *   rope      : NULL: keys are written as they are (q must then be NULL too)
+ *   q, q_out  : device [n_tokens][n_q_heads][128], or NULL both; q_out contiguous, or q itself
+ * Errors: AATC_ERR_INVALID_ARG.  n_tokens == 0 is a no-op.
+ */
+typedef struct {
+  const void* x;
+  int64_t token_stride, head_stride;   /* elements */
+} aatc_heads_t;
+aatc_status_t aatc_paged_append(const aatc_pages_t* desc, void* pages, const int32_t* table, int32_t n_rows,
+                                int32_t table_stride, int32_t max_pages, const int32_t* rows, const int32_t* index,
+                                const int32_t* positions, int32_t n_tokens, const aatc_heads_t* k,
+                                const aatc_heads_t* v, const aatc_rotary_t* rope, const aatc_heads_t* q,
+                                int32_t n_q_heads, void* q_out, int32_t* dev_flags, void* stream);
+
+/*
+ * Attention of one new token per sequence over its pages (Def. sdpa with one query row): per query head j
+ * (kv-head j / (n_q_heads / n_kv_heads)) of sequence b with n = lens[b] tokens,
+ *   s_t = scale q . k_t;  cap > 0: s_t = cap tanh(s_t / cap);  slopes: s_t += slopes[j] (t - (n - 1));
+ *   over 0 <= t < n, and t >= n - window if window > 0;
+ *   lse = ln sum_t exp(s_t), out = sum_t exp(s_t - lse) v_t.
+ * A sequence of no tokens gives out = 0, lse = -infinity.  A prior (prior_out, prior_lse) of another set
+ * of tokens, as this call or aatc_decode_attention_lse writes it, joins the same softmax.  The lengths are read on
+ * the device, so a captured call serves sequences that grow.  The tokens of all sequences are dealt out evenly
+ * over the SMs in one launch and the pieces joined in a second; fp32 softmax and sums, fp32 results.
+ *   lens      : device int32 [batch], 0 .. max_pages * page_size
+ *   q         : device [batch][n_q_heads][128], token_stride between sequences
+ *   slopes    : device fp32 [n_q_heads] or NULL
+ *   prior_out, prior_lse : device fp32 [batch][n_q_heads][128], [batch][n_q_heads], or NULL both
+ *   out, lse  : device fp32 likewise; lse may be NULL; they may be the prior itself
+ *   workspace : device, >= aatc_paged_decode_workspace_bytes, contents ignored; it does not depend on the
+ *               batch or the lengths
+ * Errors: AATC_ERR_INVALID_ARG (also n_q_heads not a multiple of n_kv_heads, batch > 65535, a cap or window
+ * below 0, a non-finite scale), AATC_ERR_WORKSPACE, AATC_ERR_CUDA.
+ */
+typedef struct {
+  float scale;              /* 1 / sqrt(128) is the usual one */
+  float cap;                /* 0: none */
+  int32_t window;           /* 0: none */
+  const float* slopes;
+  const float* prior_out;
+  const float* prior_lse;
+} aatc_paged_decode_t;
+aatc_status_t aatc_paged_decode_workspace_bytes(const aatc_pages_t* desc, int32_t n_q_heads, size_t* bytes);
+aatc_status_t aatc_paged_decode_attention(const aatc_pages_t* desc, const void* pages, const int32_t* table,
+                                          int32_t table_stride, int32_t max_pages, const int32_t* lens, int32_t batch,
+                                          const aatc_heads_t* q, int32_t n_q_heads, const aatc_paged_decode_t* how,
+                                          float* out, float* lse, void* workspace, size_t workspace_bytes,
+                                          int32_t* dev_flags, void* stream);
+
+/*
+ * Copy whole pages over n_layers layers (layer_stride bytes apart, a multiple of 16): page pairs[2 i] to
+ * page pairs[2 i + 1].  Forks get their own last page by it, compactions move pages by it.  The pairs are in
+ * host memory and are read before the call returns.
+ * Errors: AATC_ERR_INVALID_ARG, among them an id outside the pool, a page written twice, or a page both read and
+ * written (the outcome would depend on the order); n_pairs or n_layers == 0 is a no-op.  AATC_ERR_NOMEM.
+ */
+aatc_status_t aatc_pages_copy(const aatc_pages_t* desc, void* pages, int32_t n_layers, size_t layer_stride,
+                              const int32_t* pairs, int32_t n_pairs, void* stream);
+
+/*
+ * Gather tokens [first, first + n_tokens) of each of n_rows sequences out of their pages:
+ *   k_out, v_out : device [n_rows][n_tokens][n_kv_heads][128], contiguous (what aatc_encode takes)
+ *   lens         : device int32 [n_rows] or NULL; tokens at or past their sequence's length are written
+ *                  as zeros and their pages are not read
+ * Errors: AATC_ERR_INVALID_ARG, AATC_ERR_CAPACITY (first + n_tokens > max_pages * page_size).  n_tokens or n_rows
+ * == 0 is a no-op.
+ */
+aatc_status_t aatc_paged_gather(const aatc_pages_t* desc, const void* pages, const int32_t* table, int32_t n_rows,
+                                int32_t table_stride, int32_t max_pages, int32_t first, int32_t n_tokens,
+                                const int32_t* lens, void* k_out, void* v_out, int32_t* dev_flags, void* stream);
+
+/*
+ * aatc_decode_attention_sw that also writes the log of the softmax's sum, natural, over all its tokens:
+ *   lse : device fp32 [batch][n_q_heads]
+ */
+aatc_status_t aatc_decode_attention_lse(aatc_plan_t plan, int32_t layer, const void* q, const void* cache,
+                                        int32_t batch, int32_t t_first, int32_t t_end, int32_t max_tokens,
+                                        const void* k_full, const void* v_full, int32_t n_full, int32_t full_cap,
+                                        float* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

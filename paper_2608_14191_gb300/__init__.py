@@ -40,6 +40,7 @@ class Dims(ctypes.Structure):
 
 _lib = None
 _P, _I32, _SZ, _F64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_double
+_I64 = ctypes.c_int64
 
 # name -> (restype, argtypes); mirrors include/aatc.h
 SIGNATURES = {
@@ -73,6 +74,17 @@ SIGNATURES = {
     "aatc_decode_attention_noalloc": (_I32, [_P, _I32, _P, _P, _I32, _I32, _I32, _P, _P]),
     "aatc_dequantize": (_I32, [_P, _I32, _P, _I32, _I32, _I32, _I32, _P, _P]),
     "aatc_get_device_error": (_I32, [_P, ctypes.POINTER(_I32), _I32]),
+    "aatc_decode_attention_lse": (_I32, [_P, _I32, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _I32, _I32, _P, _P, _P, _SZ,
+                                         _P]),
+    "aatc_pages_bytes": (_I32, [_P, ctypes.POINTER(_SZ)]),
+    "aatc_rotary_frequencies": (_I32, [_I32, _F64, _I32, _F64, _I32, _F64, _F64, _P, _P]),
+    "aatc_rotary_turns": (_I32, [_P, _I32, _P]),
+    "aatc_rotate": (_I32, [_P, _I32, _P, _I64, _I64, _P, _I32, _I32, _I32, _P, _I64, _I64, _P]),
+    "aatc_paged_append": (_I32, [_P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _I32, _P, _P, _P, _P, _I32, _P, _P, _P]),
+    "aatc_paged_decode_workspace_bytes": (_I32, [_P, _I32, ctypes.POINTER(_SZ)]),
+    "aatc_paged_decode_attention": (_I32, [_P, _P, _P, _I32, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _SZ, _P, _P]),
+    "aatc_pages_copy": (_I32, [_P, _P, _I32, _SZ, _P, _I32, _P]),
+    "aatc_paged_gather": (_I32, [_P, _P, _P, _I32, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P]),
     "aatc_bf16_decode_workspace_bytes": (_I32, [_I32, _I32, _I32, _I32, ctypes.POINTER(_SZ)]),
     "aatc_bf16_decode_attention": (_I32, [_P, _P, _P, _I32, _I32, _I32, _I32, _I32, _P, _P, _SZ, _P]),
 }
@@ -493,10 +505,11 @@ def decode_attention(plan: Plan, layer: int, q, cache, n_ctx: int, max_tokens: i
 
 def decode_attention_sw(plan: Plan, layer: int, q, cache, t_first: int, t_end: int, max_tokens: int,
                         k_full=None, v_full=None, n_full: int = 0, out=None, workspace=None, stream=None,
-                        full_row0: int = 0):
+                        full_row0: int = 0, lse=None):
     """aatc_decode_attention_sw: packed tokens [t_first, t_end) plus the n_full tokens at rows
     [full_row0, full_row0 + n_full) of k_full / v_full (bf16 [batch][cap][H_kv][128]; the row
-    stride between sequences stays cap) in one softmax -> fp32 [batch][H_q][128]."""
+    stride between sequences stays cap) in one softmax -> fp32 [batch][H_q][128].  lse: fp32
+    [batch][H_q], gets the log of the softmax's sum (aatc_decode_attention_lse)."""
     where = "aatc_decode_attention_sw"
     _dev_tensor(q, where, "q", _BF16, 3, (None, plan.dims.n_q_heads, HEAD_DIM))
     batch = q.shape[0]
@@ -516,11 +529,18 @@ def decode_attention_sw(plan: Plan, layer: int, q, cache, t_first: int, t_end: i
     ws_ptr = None if workspace is None else _ptr(workspace)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     row_bytes = int(full_row0) * plan.dims.n_kv_heads * HEAD_DIM * 2
+    kp = None if k_full is None else _ptr(k_full) + row_bytes
+    vp = None if v_full is None else _ptr(v_full) + row_bytes
+    if lse is not None:
+        where = "aatc_decode_attention_lse"
+        _dev_tensor(lse, where, "lse", _F32, 2, (batch, plan.dims.n_q_heads))
+        _check(_lib.aatc_decode_attention_lse(plan.handle, layer, _ptr(q), _ptr(cache), batch, t_first, t_end,
+                                              max_tokens, kp, vp, int(n_full), cap, _ptr(out), _ptr(lse), ws_ptr,
+                                              ws_bytes, _stream(stream)), where)
+        return out
     _check(_lib.aatc_decode_attention_sw(plan.handle, layer, _ptr(q), _ptr(cache), batch, t_first, t_end,
-                                         max_tokens, None if k_full is None else _ptr(k_full) + row_bytes,
-                                         None if v_full is None else _ptr(v_full) + row_bytes, int(n_full), cap,
-                                         _ptr(out),
-                                         ws_ptr, ws_bytes, _stream(stream)), "aatc_decode_attention_sw")
+                                         max_tokens, kp, vp, int(n_full), cap, _ptr(out), ws_ptr, ws_bytes,
+                                         _stream(stream)), where)
     return out
 
 

@@ -228,13 +228,14 @@ cudaError_t launch_encode_hidden(const Plan& plan, int layer, const void* x, int
                                  int batch, int start, int n_tokens, void* cache, int max_tokens, cudaStream_t st);
 // Optional parts of a decode call: the packed range starts at token t_first (default 0), and
 // n_full uncompressed tokens (bf16 [batch][full_cap][n_kv][128], e.g. a full-precision sink and
-// recent window) join the same softmax.
+// recent window) join the same softmax, whose sum's logarithm is written where lse is given.
 struct DecodeExtra {
   int t_first = 0;
   const void* k_full = nullptr;
   const void* v_full = nullptr;
   int n_full = 0;
   int full_cap = 0;
+  float* lse = nullptr;       // log of the softmax's sum, fp32 [batch][n_q]
 };
 constexpr int MAX_FULL_TOKENS = 8192;   // shared-memory scores of the uncompressed tokens
 cudaError_t launch_decode(const Plan& plan, int layer, const void* q, const void* cache, int batch,

@@ -618,10 +618,11 @@ aatc_status_t aatc_decode_attention(aatc_plan_t p, int32_t layer, const void* q,
                                          workspace, static_cast<cudaStream_t>(stream), aatc::DecodeExtra{}));
 }
 
-aatc_status_t aatc_decode_attention_sw(aatc_plan_t p, int32_t layer, const void* q, const void* cache,
-                                       int32_t batch, int32_t t_first, int32_t t_end, int32_t max_tokens,
-                                       const void* k_full, const void* v_full, int32_t n_full, int32_t full_cap,
-                                       float* out, void* workspace, size_t workspace_bytes, void* stream) {
+// aatc_decode_attention_sw, and with an lse aatc_decode_attention_lse.
+static aatc_status_t decode_sw(aatc_plan_t p, int32_t layer, const void* q, const void* cache, int32_t batch,
+                               int32_t t_first, int32_t t_end, int32_t max_tokens, const void* k_full,
+                               const void* v_full, int32_t n_full, int32_t full_cap, float* out, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream) {
   aatc::Plan* plan = as_plan(p);
   if (!plan || !q || !cache || !out || layer < 0 || layer >= plan->dims.n_layers || batch < 1 ||
       max_tokens < 1 || t_first < 0 || t_end < t_first || n_full < 0 || (n_full > 0 && (!k_full || !v_full)) ||
@@ -644,8 +645,27 @@ aatc_status_t aatc_decode_attention_sw(aatc_plan_t p, int32_t layer, const void*
   ex.v_full = v_full;
   ex.n_full = n_full;
   ex.full_cap = full_cap;
+  ex.lse = lse;
   return cuda_status(aatc::launch_decode(*plan, layer, q, cache, batch, t_end, max_tokens, out, workspace,
                                          static_cast<cudaStream_t>(stream), ex));
+}
+
+aatc_status_t aatc_decode_attention_sw(aatc_plan_t p, int32_t layer, const void* q, const void* cache,
+                                       int32_t batch, int32_t t_first, int32_t t_end, int32_t max_tokens,
+                                       const void* k_full, const void* v_full, int32_t n_full, int32_t full_cap,
+                                       float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return decode_sw(p, layer, q, cache, batch, t_first, t_end, max_tokens, k_full, v_full, n_full, full_cap, out,
+                   nullptr, workspace, workspace_bytes, stream);
+}
+
+aatc_status_t aatc_decode_attention_lse(aatc_plan_t p, int32_t layer, const void* q, const void* cache,
+                                        int32_t batch, int32_t t_first, int32_t t_end, int32_t max_tokens,
+                                        const void* k_full, const void* v_full, int32_t n_full, int32_t full_cap,
+                                        float* out, float* lse, void* workspace, size_t workspace_bytes,
+                                        void* stream) {
+  if (!lse || (reinterpret_cast<uintptr_t>(lse) & 3u)) return AATC_ERR_INVALID_ARG;
+  return decode_sw(p, layer, q, cache, batch, t_first, t_end, max_tokens, k_full, v_full, n_full, full_cap, out, lse,
+                   workspace, workspace_bytes, stream);
 }
 
 aatc_status_t aatc_dequantize(aatc_plan_t p, int32_t layer, const void* cache, int32_t batch,

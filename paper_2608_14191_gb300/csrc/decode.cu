@@ -94,6 +94,7 @@ struct DecodeArgs {
   const __nv_bfloat16* k_full;  // uncompressed tokens attended as well: [batch][full_cap][n_kv][128]
   const __nv_bfloat16* v_full;
   int n_full, full_cap;
+  float* lse;               // [batch][HQ] or null: log of the softmax's sum
   int n_stages;             // fused kernel: tile ring depth
   int stage_bytes, nks_max; // fused kernel: bytes of a ring stage, score k-steps of the layer's widest streams
 };
@@ -1541,7 +1542,9 @@ __global__ void __launch_bounds__(kMThreads, PER_SM)
   const float Mt = fmaxf(M, m_f);
   const float ap = a.n_splits > 0 ? fast_exp2(M - Mt) : 0.0f;
   const float af = a.n_full > 0 ? fast_exp2(m_f - Mt) : 0.0f;
-  const float inv_den = 1.0f / fmaf(L, ap, l_f * af);
+  const float den = fmaf(L, ap, l_f * af), inv_den = 1.0f / den;
+  if (a.lse && tid == 0 && blockIdx.x % PARTS == 0)
+    a.lse[static_cast<size_t>(b) * a.n_q + j] = (Mt + log2f(den)) * 0.6931471805599453f;   // ln 2
   if (tid < D) {
     float o = 0.0f;
     if (a.n_splits > 0 && M > -INFINITY) {
@@ -2000,6 +2003,7 @@ cudaError_t launch_decode(const Plan& plan, int layer, const void* q, const void
   a.v_full = static_cast<const __nv_bfloat16*>(extra.v_full);
   a.n_full = extra.n_full;
   a.full_cap = extra.full_cap;
+  a.lse = extra.lse;
   const int np = (a.group + 3) / 4;
   const DecodeRoute route = decode_route(plan, layer, batch, n_ctx, extra.t_first, extra.n_full);
   const FusedChoice& fk = route.fused;
