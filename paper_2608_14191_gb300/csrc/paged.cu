@@ -119,100 +119,512 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
 }
 
 // ---------------------------------------------------------------- decode attention
-constexpr int kHeadsPerCta = 8;     // query heads of one kv-head that a CTA takes
-constexpr int kDecodeThreads = 256;
+// The work of a call is its units of 16 tokens: those of sequence 0's kv-head 0, then kv-head 1, ...,
+// then sequence 1's, a (sequence, kv-head) being a segment.  CTA c of n takes the units
+// [c U / n, (c + 1) U / n) of all U, so every CTA has the same share whatever the lengths; a segment
+// that lies inside one CTA's share is finished there, the pieces of any other go to the workspace and are joined
+// by the second launch.  (Query heads beyond eight of a kv-head are further segments over the same tokens.)
+constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
+constexpr int kUnit = 16;           // tokens
+constexpr int kDecodeWarps = 4;
+constexpr int kDecodeCtas = 3;      // per SM
+constexpr int kUnitsPerCta = 4;     // fewer CTAs where they would get less
+constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128], maxima [8], totals [8]
 
-// One CTA per (sequence, kv-head, eight of its query heads): a warp takes every eighth token, a lane four of
-// its dimensions, with an online softmax per warp; the warps are joined in shared memory.
+// Workspace: pieces [2 n_ctas] (CTA c's share begins inside a segment: piece 2 c; ends inside one that it began:
+// 2 c + 1), then int4 per CTA: the segment that it began and did not end (sequence, segment of the
+// sequence, last CTA with a piece of it; sequence -1: none).
+struct Share {
+  int64_t total;                    // units
+  int n_ctas;                       // CTAs that get any
+};
+
 template <typename T>
-__global__ void __launch_bounds__(kDecodeThreads) aatc_paged_decode_kernel(const DecodeArgs a) {
-  constexpr int kW = kDecodeThreads / 32, G = kHeadsPerCta;
-  __shared__ float so[kW][G][D];
-  __shared__ float sm[kW][G], sl[kW][G];
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                    uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                                   uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma<__half>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                            uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of an 8 x 8 matrix of 16-bit values over the warp
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float exp2_of(float x) {            // (-inf: 0)
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint4 load_once(const char* p) {    // 16 bytes that are read once
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+
+// A weight p as a sum of 16-bit values, so that products with 16-bit values on the tensor cores lose
+// nothing of it: bf16, three truncations of eight significant bits (all of p's 24); f16, a truncation and the
+// rounded rest (22 bits; p <= 2^14 and its scale keep the rest above the format's smallest step for
+// any p over 2^-30 of the largest).  No part is negative, and no bf16 part zero, as an infinite value
+// times it would turn into NaN.
+template <typename T>
+struct Parts;
+template <>
+struct Parts<__nv_bfloat16> {
+  static constexpr int kN = 3;
+  static constexpr float kShift = 0.0f;                        // log2 of the scale on p
+  static __device__ __forceinline__ void split(float p, float q, uint32_t (&out)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const uint32_t a = __float_as_uint(p), b = __float_as_uint(q);
+      out[i] = __byte_perm(a, b, 0x7632);
+      p = fmaxf(p - __uint_as_float(a & 0xFFFF0000u), 7.8886e-31f);   // about 2^-100
+      q = fmaxf(q - __uint_as_float(b & 0xFFFF0000u), 7.8886e-31f);
+    }
+  }
+};
+template <>
+struct Parts<__half> {
+  static constexpr int kN = 2;
+  static constexpr float kShift = 6.0f;
+  static __device__ __forceinline__ void split(float p, float q, uint32_t (&out)[2]) {
+    const __half2 h = __halves2half2(__float2half_rz(p), __float2half_rz(q));
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(p - f.x, q - f.y);
+    out[0] = *reinterpret_cast<const uint32_t*>(&h);
+    out[1] = *reinterpret_cast<const uint32_t*>(&l);
+  }
+};
+
+// First token and unit count of a sequence: the tokens [lo, n) in units from lo / 16 on; one unit, of nothing,
+// for an empty one (somebody has to write its result).
+struct Extent {
+  int n, lo, units;
+};
+__device__ __forceinline__ Extent extent_of(const DecodeArgs& a, int b) {
+  Extent e;
+  e.n = min(max(a.lens[b], 0), a.pool.max_pages << a.pool.page_shift);
+  e.lo = a.window > 0 ? max(0, e.n - a.window) : 0;
+  e.units = max(1, (e.n + kUnit - 1) / kUnit - e.lo / kUnit);
+  return e;
+}
+
+__device__ __forceinline__ int segments_of(const DecodeArgs& a) {
+  return a.pool.n_kv * ((a.group + kSegHeads - 1) / kSegHeads);
+}
+
+// Unit u of all is in the share of CTA ((u + 1) n - 1) / U.
+__device__ __forceinline__ int cta_of(const Share& s, int64_t unit) {
+  return static_cast<int>(((unit + 1) * s.n_ctas - 1) / s.total);
+}
+
+// K and V fragments of a unit.  Lane (g, t) = (lane / 4, lane % 4) holds of K the tokens g and g + 8,
+// dimensions 32 j + 8 t .. + 7 (A operand of the score MMAs: rows are tokens, the order of the
+// dimensions is free as long as the query's is the same), and of V the tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9,
+// dimensions 8 g .. + 7 and 64 + 8 g .. + 7 (A operand of the output MMAs after pairs of tokens are
+// interleaved: rows are dimensions).  Every load is of 16 bytes, whole 32-byte sectors, straight to registers.
+struct Kreg {
+  uint4 r[2][4];                    // [token half][j]
+};
+struct Vreg {
+  uint4 r[2][2][2];                 // [token half][token][dimension half]
+};
+
+// Where a unit's tokens lie.
+struct Place {
+  const char* half[2];              // keys of tokens 0 .. 7 and 8 .. 15 of the unit (null: none is live)
+  int live_lo, live_hi;             // live tokens of the unit
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_decode_kernel(const DecodeArgs a) {
+  constexpr int kW = kDecodeWarps, kT = kW * 32;
+  static_assert(kT == D, "a thread per dimension joins the warps");
+  __shared__ float so[kW][kSegHeads][D];
+  __shared__ float sm[kW][kSegHeads], sl[kW][kSegHeads];
+  __shared__ int64_t s_part[kW];
+  __shared__ int64_t s_before;
+  __shared__ int s_seq;
   const Pool& p = a.pool;
-  const int blocks = (a.group + G - 1) / G;
-  const int h = blockIdx.x / blocks, g0 = (blockIdx.x % blocks) * G, n_g = min(G, a.group - g0);
-  const int b = blockIdx.y, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  int n = a.lens[b];
-  if (n < 0 || n > p.max_pages << p.page_shift) {
-    if (threadIdx.x == 0) raise(p.err, kBadRow);
-    n = min(max(n, 0), p.max_pages << p.page_shift);
-  }
-  const int lo = a.window > 0 ? max(0, n - a.window) : 0;
-  float q[G][4], o[G][4], m[G], l[G];
-  const int j0 = h * a.group + g0;
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    m[g] = -INFINITY;
-    l[g] = 0.0f;
-    uint2 w = make_uint2(0, 0);
-    if (g < n_g)
-      w = *reinterpret_cast<const uint2*>(static_cast<const T*>(a.q.x) + b * a.q.token_stride + (j0 + g) * a.q.head_stride +
-                                          4 * lane);
-    const float2 x = widen(T(), w.x), y = widen(T(), w.y);
-    q[g][0] = x.x; q[g][1] = x.y; q[g][2] = y.x; q[g][3] = y.y;
-    o[g][0] = o[g][1] = o[g][2] = o[g][3] = 0.0f;
-  }
-  for (int t = lo + warp; t < n; t += kW) {
-    const int32_t id = p.table[static_cast<int64_t>(b) * p.table_stride + (t >> p.page_shift)];
-    if (id < 0 || id >= p.n_pages) {
-      if (lane == 0) raise(p.err, kBadPage);
-      continue;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t4 = lane % 4;
+  const int n_seg = segments_of(a), seg_blocks = (a.group + kSegHeads - 1) / kSegHeads;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+
+  // ---- this CTA's share: the total, then the sequence in which the share begins
+  Share share;
+  int64_t first = 0, last = 0, seq_start = 0;       // units of all; first of sequence b
+  int b = 0;
+  {
+    int64_t mine = 0;
+    for (int i = tid; i < a.batch; i += kT) {
+      mine += extent_of(a, i).units;
+      const int n = a.lens[i];
+      if (blockIdx.x == 0 && (n < 0 || n > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
     }
-    const T* k = static_cast<const T*>(p.pages) + (((static_cast<int64_t>(id) * 2 * p.n_kv + h) << p.page_shift) +
-                                                   (t & ((1 << p.page_shift) - 1))) * D + 4 * lane;
-    const T* v = k + (static_cast<int64_t>(p.n_kv) << p.page_shift) * D;
-    const uint2 kw = *reinterpret_cast<const uint2*>(k), vw = *reinterpret_cast<const uint2*>(v);
-    const float2 k0 = widen(T(), kw.x), k1 = widen(T(), kw.y), v0 = widen(T(), vw.x), v1 = widen(T(), vw.y);
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      if (g >= n_g) break;
-      float s = q[g][0] * k0.x + q[g][1] * k0.y + q[g][2] * k1.x + q[g][3] * k1.y;
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (lane == 0) s_part[warp] = mine;
+    __syncthreads();
+    share.total = 0;
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-      s *= a.scale;
-      if (a.cap > 0.0f) s = a.cap * tanhf(s / a.cap);
-      if (a.slopes) s += a.slopes[j0 + g] * static_cast<float>(t - (n - 1));
-      const float mn = fmaxf(m[g], s), base = mn == -INFINITY ? 0.0f : mn;
-      const float r = exp2f((m[g] - base) * kLog2e), e = exp2f((s - base) * kLog2e);
-      m[g] = mn;
-      l[g] = l[g] * r + e;
-      o[g][0] = o[g][0] * r + e * v0.x;
-      o[g][1] = o[g][1] * r + e * v0.y;
-      o[g][2] = o[g][2] * r + e * v1.x;
-      o[g][3] = o[g][3] * r + e * v1.y;
+    for (int w = 0; w < kW; ++w) share.total += s_part[w];
+    share.total *= n_seg;
+    share.n_ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (share.total + kUnitsPerCta - 1) / kUnitsPerCta));
+    int4* desc = reinterpret_cast<int4*>(a.ws + static_cast<size_t>(gridDim.x) * 2 * kPiece);
+    if (tid == 0) desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (blockIdx.x >= share.n_ctas) return;
+    first = blockIdx.x * share.total / share.n_ctas;
+    last = (blockIdx.x + 1) * share.total / share.n_ctas;
+    // prefix sums over the sequences, kT at a time, until one passes `first`
+    __syncthreads();
+    int64_t before = 0;
+    for (int i0 = 0; i0 < a.batch; i0 += kT) {
+      const int i = i0 + tid;
+      const int64_t units = i < a.batch ? static_cast<int64_t>(extent_of(a, i).units) * n_seg : 0;
+      int64_t upto = units;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      if (lane == 31) s_part[warp] = upto;
+      __syncthreads();
+      int64_t total = before;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        if (w == warp) upto += total;
+        total += s_part[w];
+      }
+      if (units > 0 && upto > first && upto - units <= first) {
+        s_seq = i;
+        s_before = upto - units;
+      }
+      __syncthreads();
+      before = total;
+      if (before > first) break;
     }
+    b = s_seq;
+    seq_start = s_before;
   }
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    *reinterpret_cast<float4*>(&so[warp][g][4 * lane]) = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
-    if (lane == 0) {
-      sm[warp][g] = m[g];
-      sl[warp][g] = l[g];
+
+  int64_t at = first;
+  Extent ext = extent_of(a, b);
+  while (at < last) {
+    if (at >= seq_start + static_cast<int64_t>(ext.units) * n_seg) {
+      seq_start += static_cast<int64_t>(ext.units) * n_seg;
+      ext = extent_of(a, ++b);
     }
+    const int seg = static_cast<int>((at - seq_start) / ext.units);
+    const int64_t seg_start = seq_start + static_cast<int64_t>(seg) * ext.units;
+    const int u0 = static_cast<int>(at - seg_start);
+    const int u1 = static_cast<int>(min(static_cast<int64_t>(ext.units), last - seg_start));
+    const int h = seg / seg_blocks, head0 = h * a.group + (seg % seg_blocks) * kSegHeads;
+    const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
+    const int32_t* row = p.table + static_cast<int64_t>(b) * p.table_stride;
+
+    // ---- the queries: B operand of the score MMAs, column g
+    uint32_t qf[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (g < n_g)
+        w = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q.x) + b * a.q.token_stride +
+                                            (head0 + g) * a.q.head_stride + 32 * j + 8 * t4);
+      qf[j][0] = w.x; qf[j][1] = w.y; qf[j][2] = w.z; qf[j][3] = w.w;
+    }
+    float slope0 = 0.0f, slope1 = 0.0f;
+    if (a.slopes) {
+      if (2 * t4 < n_g) slope0 = a.slopes[head0 + 2 * t4] * kLog2e;
+      if (2 * t4 + 1 < n_g) slope1 = a.slopes[head0 + 2 * t4 + 1] * kLog2e;
+    }
+    float acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+
+    const int unit0 = ext.lo / kUnit;
+    const int64_t v_off = (static_cast<int64_t>(p.n_kv) << p.page_shift) * (D * 2);
+    auto ids_of = [&](int u, int2& id) {             // (u may be past the end: not read then)
+      const int t = (unit0 + u) * kUnit;
+      id = make_int2(-1, -1);
+      if (u < u1 && t < ext.n) {
+        id.x = __ldg(row + (t >> p.page_shift));
+        id.y = p.page_shift > 3 ? id.x : t + 8 < ext.n ? __ldg(row + ((t + 8) >> p.page_shift)) : -1;
+      }
+    };
+    auto place_of = [&](int u, const int2& id) {
+      const int t = (unit0 + u) * kUnit;
+      Place pl;
+      pl.live_lo = max(0, ext.lo - t);
+      pl.live_hi = u < u1 ? min(kUnit, ext.n - t) : 0;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int one = e ? id.y : id.x;
+        const bool live = pl.live_hi > 8 * e && pl.live_lo < 8 * e + 8;
+        const bool good = static_cast<uint32_t>(one) < static_cast<uint32_t>(p.n_pages);
+        if (live && !good && lane == 0) raise(p.err, kBadPage);
+        pl.half[e] = live && good ? static_cast<const char*>(p.pages) +
+                                        (((static_cast<int64_t>(one) * 2 * p.n_kv + h) << p.page_shift) +
+                                         ((t + 8 * e) & ((1 << p.page_shift) - 1))) * (D * 2)
+                                  : nullptr;
+      }
+      return pl;
+    };
+    auto load_k = [&](const Place& pl, Kreg& k) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const bool in = pl.half[e] && 8 * e + g >= pl.live_lo && 8 * e + g < pl.live_hi;
+        const char* src = pl.half[e] + g * (D * 2) + 16 * t4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k.r[e][j] = in ? load_once(src + 64 * j) : make_uint4(0, 0, 0, 0);
+      }
+    };
+    auto load_v = [&](const Place& pl, Vreg& v) {    // (a masked token's weight is 0, and 0 x NaN is not)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int tok = 8 * e + 2 * t4 + i;
+          const bool in = pl.half[e] && tok >= pl.live_lo && tok < pl.live_hi;
+          const char* src = pl.half[e] + v_off + (2 * t4 + i) * (D * 2) + 16 * g;
+#pragma unroll
+          for (int d = 0; d < 2; ++d) v.r[e][i][d] = in ? load_once(src + 128 * d) : make_uint4(0, 0, 0, 0);
+        }
+    };
+
+    int u = u0 + warp;
+    int2 id, id_next;
+    ids_of(u, id);
+    ids_of(u + kW, id_next);
+    Place pl = place_of(u, id);
+    Kreg k;
+    Vreg v;
+    load_k(pl, k);
+    load_v(pl, v);
+    for (; u < u1; u += kW) {
+      float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        mma<T>(s, k.r[0][j].x, k.r[1][j].x, k.r[0][j].y, k.r[1][j].y, qf[j][0], qf[j][1]);
+        mma<T>(s, k.r[0][j].z, k.r[1][j].z, k.r[0][j].w, k.r[1][j].w, qf[j][2], qf[j][3]);
+      }
+      const Place here = pl;
+      pl = place_of(u + kW, id_next);
+      load_k(pl, k);
+      ids_of(u + 2 * kW, id_next);
+      // ---- scores in units of ln 2: s[0], s[1] token g, s[2], s[3] token g + 8; queries 2 t4, 2 t4 + 1
+      const int tok = (unit0 + u) * kUnit + g;
+      if (a.cap > 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = a.cap * kLog2e * tanhf(s[i] * a.scale / a.cap);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] *= a.scale * kLog2e;
+      }
+      if (a.slopes) {
+        const float back0 = static_cast<float>(tok - (ext.n - 1)), back1 = static_cast<float>(tok + 8 - (ext.n - 1));
+        s[0] = fmaf(slope0, back0, s[0]);
+        s[1] = fmaf(slope1, back0, s[1]);
+        s[2] = fmaf(slope0, back1, s[2]);
+        s[3] = fmaf(slope1, back1, s[3]);
+      }
+      if (!here.half[0] || g < here.live_lo || g >= here.live_hi) s[0] = s[1] = -INFINITY;
+      if (!here.half[1] || g + 8 < here.live_lo || g + 8 >= here.live_hi) s[2] = s[3] = -INFINITY;
+      // ---- the running reference of the exponents follows the maximum only when that is 2^8 past it
+      const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
+      if (__any_sync(0xffffffffu, top0 > m0 + 8.0f || top1 > m1 + 8.0f)) {
+        float n0 = fmaxf(m0, top0), n1 = fmaxf(m1, top1);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, o));
+          n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, o));
+        }
+        const float r0 = n0 == -INFINITY ? 1.0f : exp2_of(m0 - n0), r1 = n1 == -INFINITY ? 1.0f : exp2_of(m1 - n1);
+        m0 = n0;
+        m1 = n1;
+        l0 *= r0;
+        l1 *= r1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          acc[i][0] *= r0;
+          acc[i][1] *= r1;
+          acc[i][2] *= r0;
+          acc[i][3] *= r1;
+        }
+      }
+      const float base0 = m0 == -INFINITY ? 0.0f : m0 - Parts<T>::kShift;
+      const float base1 = m1 == -INFINITY ? 0.0f : m1 - Parts<T>::kShift;
+      s[0] = exp2_of(s[0] - base0);
+      s[1] = exp2_of(s[1] - base1);
+      s[2] = exp2_of(s[2] - base0);
+      s[3] = exp2_of(s[3] - base1);
+      l0 += s[0] + s[2];
+      l1 += s[1] + s[3];
+      uint32_t w[2][Parts<T>::kN];
+      Parts<T>::split(s[0], s[1], w[0]);
+      Parts<T>::split(s[2], s[3], w[1]);
+#pragma unroll
+      for (int i = 0; i < Parts<T>::kN; ++i) {
+        w[0][i] = transposed(w[0][i]);
+        w[1][i] = transposed(w[1][i]);
+      }
+      // ---- rows 8 g + i and 64 + 8 g + i of V^T
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t f[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int d = 0; d < 2; ++d) {
+            const uint32_t x = reinterpret_cast<const uint32_t*>(&v.r[e][0][d])[i / 2];
+            const uint32_t y = reinterpret_cast<const uint32_t*>(&v.r[e][1][d])[i / 2];
+            f[2 * e + d] = __byte_perm(x, y, i % 2 ? 0x7632 : 0x5410);
+          }
+#pragma unroll
+        for (int x = 0; x < Parts<T>::kN; ++x) mma<T>(acc[i], f[0], f[1], f[2], f[3], w[0][x], w[1][x]);
+      }
+      load_v(pl, v);
+    }
+
+    // ---- join the warps
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      l0 += __shfl_xor_sync(0xffffffffu, l0, o);
+      l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+    }
+    if (g == 0) {
+      sm[warp][2 * t4] = m0;
+      sm[warp][2 * t4 + 1] = m1;
+      sl[warp][2 * t4] = l0;
+      sl[warp][2 * t4 + 1] = l1;
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        float* to = &so[warp][2 * t4 + c][64 * d + 8 * g];
+        const int x = 2 * d + c;
+        *reinterpret_cast<float4*>(to) = make_float4(acc[0][x], acc[1][x], acc[2][x], acc[3][x]);
+        *reinterpret_cast<float4*>(to + 4) = make_float4(acc[4][x], acc[5][x], acc[6][x], acc[7][x]);
+      }
+    __syncthreads();
+    const bool begins = u0 == 0, ends = u1 == ext.units;
+    float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + (begins ? 1 : 0)) * kPiece;
+    for (int q = 0; q < n_g; ++q) {
+      const int64_t out_row = static_cast<int64_t>(b) * a.n_q + head0 + q;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) top = fmaxf(top, sm[w][q]);
+      const bool whole = begins && ends;
+      const float prior = whole && a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
+      top = fmaxf(top, prior);
+      const float base = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f, total = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        const float f = exp2_of(sm[w][q] - base);
+        sum = fmaf(f, so[w][q][tid], sum);
+        total = fmaf(f, sl[w][q], total);
+      }
+      sum *= exp2f(-Parts<T>::kShift);
+      total *= exp2f(-Parts<T>::kShift);
+      if (whole) {
+        if (prior > -INFINITY) {
+          const float f = exp2_of(prior - base);
+          sum = fmaf(f, a.prior_out[out_row * D + tid], sum);
+          total += f;
+        }
+        a.out[out_row * D + tid] = total == 0.0f ? 0.0f : sum / total;
+        __syncthreads();                             // (the log-sum may be written over the prior's)
+        if (a.lse && tid == 0) a.lse[out_row] = base * kLn2 + logf(total);
+      } else {
+        piece[q * D + tid] = sum;
+        if (tid == 0) {
+          piece[kSegHeads * D + q] = top;
+          piece[kSegHeads * D + kSegHeads + q] = total;
+        }
+      }
+    }
+    if (begins && !ends && tid == 0) {
+      int4* desc = reinterpret_cast<int4*>(a.ws + static_cast<size_t>(gridDim.x) * 2 * kPiece);
+      desc[blockIdx.x] = make_int4(b, seg, cta_of(share, seg_start + ext.units - 1), 0);
+    }
+    __syncthreads();
+    at = seg_start + u1;
   }
+}
+
+// Joins the pieces of the segments that CTA blockIdx.x of the first launch began and did not end; one CTA
+// a query head, a warp takes every eighth piece, a lane four dimensions.
+constexpr int kJoinWarps = 8;
+__global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const DecodeArgs a, int n_ctas) {
+  __shared__ float so[kJoinWarps][D];
+  __shared__ float sm[kJoinWarps], sl[kJoinWarps];
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int4 what = __ldcg(reinterpret_cast<const int4*>(a.ws + static_cast<size_t>(n_ctas) * 2 * kPiece) + blockIdx.x);
+  if (what.x < 0) return;
+  const int seg_blocks = (a.group + kSegHeads - 1) / kSegHeads, h = what.y / seg_blocks;
+  const int head = h * a.group + (what.y % seg_blocks) * kSegHeads + blockIdx.y;
+  if (head >= (h + 1) * a.group) return;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, q = blockIdx.y;
+  const int c0 = blockIdx.x, n = what.z - c0 + 1;                // pieces 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
+  float top = -INFINITY, total = 0.0f;
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int i = warp; i < n; i += kJoinWarps) {
+    const float* piece = a.ws + (static_cast<size_t>(c0 + i) * 2 + (i == 0 ? 1 : 0)) * kPiece;
+    const float m = __ldcg(piece + kSegHeads * D + q), l = __ldcg(piece + kSegHeads * D + kSegHeads + q);
+    const float4 o = __ldcg(reinterpret_cast<const float4*>(piece + q * D) + lane);
+    const float next = fmaxf(top, m), base = next == -INFINITY ? 0.0f : next;
+    const float r = exp2_of(top - base), f = exp2_of(m - base);
+    total = fmaf(total, r, f * l);
+    sum.x = fmaf(sum.x, r, f * o.x);
+    sum.y = fmaf(sum.y, r, f * o.y);
+    sum.z = fmaf(sum.z, r, f * o.z);
+    sum.w = fmaf(sum.w, r, f * o.w);
+    top = next;
+  }
+  *reinterpret_cast<float4*>(&so[warp][4 * lane]) = sum;
+  if (lane == 0) {
+    sm[warp] = top;
+    sl[warp] = total;
+  }
+  const int64_t out_row = static_cast<int64_t>(what.x) * a.n_q + head;
+  const float prior = a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
   __syncthreads();
-  for (int i = threadIdx.x; i < n_g * D; i += kDecodeThreads) {
-    const int g = i / D, d = i % D;
-    const int64_t row = static_cast<int64_t>(b) * a.n_q + j0 + g;
-    float top = a.prior_lse ? a.prior_lse[row] : -INFINITY;
-    for (int w = 0; w < kW; ++w) top = fmaxf(top, sm[w][g]);
-    const float base = top == -INFINITY ? 0.0f : top;
-    float total = 0.0f, acc = 0.0f;
-    if (a.prior_lse) {
-      total = exp2f((a.prior_lse[row] - base) * kLog2e);
-      if (total > 0.0f) acc = total * a.prior_out[row * D + d];
-    }
-    for (int w = 0; w < kW; ++w) {
-      const float f = exp2f((sm[w][g] - base) * kLog2e);
-      total += f * sl[w][g];
-      acc += f * so[w][g][d];
-    }
-    a.out[row * D + d] = total == 0.0f ? 0.0f : acc / total;
-    if (a.lse) so[0][g][d] = base + logf(total);
+  if (tid >= D) return;
+  top = prior;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, sm[w]);
+  const float base = top == -INFINITY ? 0.0f : top;
+  float s = 0.0f, l = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float f = exp2_of(sm[w] - base);
+    s = fmaf(f, so[w][tid], s);
+    l = fmaf(f, sl[w], l);
   }
-  __syncthreads();
-  if (a.lse && threadIdx.x < n_g) a.lse[static_cast<int64_t>(b) * a.n_q + j0 + threadIdx.x] = so[0][threadIdx.x][0];
+  if (prior > -INFINITY) {
+    const float f = exp2_of(prior - base);
+    s = fmaf(f, a.prior_out[out_row * D + tid], s);
+    l += f;
+  }
+  a.out[out_row * D + tid] = l == 0.0f ? 0.0f : s / l;
+  if (a.lse && tid == 0) a.lse[out_row] = base * kLn2 + logf(l);   // (every thread has read the prior's)
 }
 
 // ---------------------------------------------------------------- page copies
@@ -259,13 +671,17 @@ cudaError_t launch_append(int dtype, const AppendArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-size_t decode_workspace(int, int, int) { return 0; }
+size_t decode_workspace(int num_sms) {
+  const size_t ctas = static_cast<size_t>(std::max(1, num_sms)) * kDecodeCtas;
+  return ctas * (2 * kPiece * sizeof(float) + sizeof(int4));
+}
 
 cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
-  const dim3 grid(a.pool.n_kv * ((a.group + kHeadsPerCta - 1) / kHeadsPerCta), a.batch);
-  if (dtype == AATC_BF16) aatc_paged_decode_kernel<__nv_bfloat16><<<grid, kDecodeThreads, 0, st>>>(a);
-  else aatc_paged_decode_kernel<__half><<<grid, kDecodeThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  const int ctas = std::max(1, a.num_sms) * kDecodeCtas;
+  const auto kernel = dtype == AATC_BF16 ? aatc_paged_decode_kernel<__nv_bfloat16> : aatc_paged_decode_kernel<__half>;
+  const cudaError_t e = launch_pdl(kernel, dim3(ctas), dim3(kDecodeWarps * 32), 0, st, a);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(aatc_paged_join_kernel, dim3(ctas, std::min(a.group, kSegHeads)), dim3(kJoinWarps * 32), 0, st, a, ctas);
 }
 
 cudaError_t launch_copy(void* pages, size_t page_bytes, int n_layers, size_t layer_stride, const int32_t* pairs,

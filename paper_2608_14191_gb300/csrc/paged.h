@@ -86,7 +86,7 @@ struct CopyPairs {
 };
 
 cudaError_t launch_append(int dtype, const AppendArgs& a, cudaStream_t st);
-size_t decode_workspace(int n_kv, int n_q, int num_sms);
+size_t decode_workspace(int num_sms);
 cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st);
 // pairs: host (source, destination) ids, checked
 cudaError_t launch_copy(void* pages, size_t page_bytes, int n_layers, size_t layer_stride, const int32_t* pairs,

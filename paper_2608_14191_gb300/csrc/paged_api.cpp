@@ -192,7 +192,7 @@ aatc_status_t aatc_paged_decode_workspace_bytes(const aatc_pages_t* desc, int32_
   int sms = 0;
   const cudaError_t e = sm_count(&sms);
   if (e != cudaSuccess) return status_from_cuda(e);
-  *bytes = paged::decode_workspace(desc->n_kv_heads, n_q_heads, sms);
+  *bytes = paged::decode_workspace(sms);
   return AATC_OK;
 }
 
@@ -212,7 +212,7 @@ aatc_status_t aatc_paged_decode_attention(const aatc_pages_t* desc, const void* 
   int sms = 0;
   const cudaError_t e = sm_count(&sms);
   if (e != cudaSuccess) return status_from_cuda(e);
-  const size_t need = paged::decode_workspace(desc->n_kv_heads, n_q_heads, sms);
+  const size_t need = paged::decode_workspace(sms);
   if (workspace_bytes < need || (need && !workspace)) return AATC_ERR_WORKSPACE;
   paged::DecodeArgs a = {};
   a.pool = pool(desc, const_cast<void*>(pages), table, table_stride, max_pages, dev_flags);
