@@ -121,9 +121,13 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
 // ---------------------------------------------------------------- decode attention
 // The work of a call is its units of 16 tokens: those of sequence 0's kv-head 0, then kv-head 1, ...,
 // then sequence 1's, a (sequence, kv-head) being a segment.  CTA c of n takes the units
-// [c U / n, (c + 1) U / n) of all U, so every CTA has the same share whatever the lengths; a segment
-// that lies inside one CTA's share is finished there, the pieces of any other go to the workspace and are joined
-// by the second launch.  (Query heads beyond eight of a kv-head are further segments over the same tokens.)
+// [c U / n, (c + 1) U / n) of all U and each of its warps a quarter of those, so every warp has the same
+// share whatever the lengths.  A segment that lies inside a warp's share is finished by the warp, the pieces of one
+// that lies in several warps are joined in shared memory, and those of one in several CTAs
+// through the workspace by the second launch.  (Query heads beyond eight of a kv-head are further segments over
+// the same tokens.)  A warp's loads run ahead of its sums across the segments of its share: with
+// shares by CTA and a barrier per segment, 61 sequences of 62 to 4001 tokens took twice as long as as many tokens
+// in equal sequences.
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
 constexpr int kDecodeWarps = 4;
@@ -214,16 +218,12 @@ struct Parts<__half> {
 struct Extent {
   int n, lo, units;
 };
-__device__ __forceinline__ Extent extent_of(const DecodeArgs& a, int b) {
+__device__ __forceinline__ Extent extent_of(const DecodeArgs& a, int len) {
   Extent e;
-  e.n = min(max(a.lens[b], 0), a.pool.max_pages << a.pool.page_shift);
+  e.n = min(max(len, 0), a.pool.max_pages << a.pool.page_shift);
   e.lo = a.window > 0 ? max(0, e.n - a.window) : 0;
   e.units = max(1, (e.n + kUnit - 1) / kUnit - e.lo / kUnit);
   return e;
-}
-
-__device__ __forceinline__ int segments_of(const DecodeArgs& a) {
-  return a.pool.n_kv * ((a.group + kSegHeads - 1) / kSegHeads);
 }
 
 // Unit u of all is in the share of CTA ((u + 1) n - 1) / U.
@@ -243,191 +243,208 @@ struct Vreg {
   uint4 r[2][2][2];                 // [token half][token][dimension half]
 };
 
-// Where a unit's tokens lie.
-struct Place {
-  const char* half[2];              // keys of tokens 0 .. 7 and 8 .. 15 of the unit (null: none is live)
-  int live_lo, live_hi;             // live tokens of the unit
+// A unit on its way through a warp: where it belongs, and the ids of the pages of its two halves.
+struct Unit {
+  int b, seg, u, t;                 // sequence, segment of it, unit of the segment, first token
+  Extent ext;
+  int id[2];
+};
+
+// A warp's piece of a segment that it does not have whole, in shared memory.
+struct Piece {
+  float sum[kSegHeads][D];
+  float top[kSegHeads], total[kSegHeads];
+};
+struct PieceOf {
+  int b, seg;                       // b < 0: none
+  int ends;
+  int64_t last_unit;                // of the segment, among all units
 };
 
 template <typename T>
 __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_decode_kernel(const DecodeArgs a) {
   constexpr int kW = kDecodeWarps, kT = kW * 32;
   static_assert(kT == D, "a thread per dimension joins the warps");
-  __shared__ float so[kW][kSegHeads][D];
-  __shared__ float sm[kW][kSegHeads], sl[kW][kSegHeads];
-  __shared__ int64_t s_part[kW];
-  __shared__ int64_t s_before;
-  __shared__ int s_seq;
+  constexpr float kUnshift = 1.0f / (1 << static_cast<int>(Parts<T>::kShift));
+  __shared__ Piece s_piece[kW][2];                   // [0]: of a segment begun before the warp's share
+  __shared__ PieceOf s_of[kW][2];
+  __shared__ int64_t s_part[kW], s_before[kW];
+  __shared__ int s_seq[kW], s_len[kW];
   const Pool& p = a.pool;
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t4 = lane % 4;
-  const int n_seg = segments_of(a), seg_blocks = (a.group + kSegHeads - 1) / kSegHeads;
+  const int tid = threadIdx.x, warp = ptx::warp_uniform(tid / 32), lane = tid % 32, g = lane / 4, t4 = lane % 4;
+  const int seg_blocks = (a.group + kSegHeads - 1) / kSegHeads, n_seg = p.n_kv * seg_blocks;
+  int4* desc = reinterpret_cast<int4*>(a.ws + static_cast<size_t>(gridDim.x) * 2 * kPiece);
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
 
-  // ---- this CTA's share: the total, then the sequence in which the share begins
-  Share share;
-  int64_t first = 0, last = 0, seq_start = 0;       // units of all; first of sequence b
-  int b = 0;
-  {
-    int64_t mine = 0;
-    for (int i = tid; i < a.batch; i += kT) {
-      mine += extent_of(a, i).units;
-      const int n = a.lens[i];
-      if (blockIdx.x == 0 && (n < 0 || n > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
+  // ---- the total, and the sequences in which the warps' shares begin: prefix sums over kT sequences at a time
+  int len = 0;
+  int64_t units = 0, upto = 0;                       // of sequence i0 + tid; up to it within the chunk
+  auto scan = [&](int i0) {
+    const int i = i0 + tid;
+    len = i < a.batch ? __ldg(a.lens + i) : 0;
+    units = i < a.batch ? static_cast<int64_t>(extent_of(a, len).units) * n_seg : 0;
+    upto = units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    if (lane == 0) s_part[warp] = mine;
+    __syncthreads();                                 // (the last chunk's sums have been read)
+    if (lane == 31) s_part[warp] = upto;
     __syncthreads();
-    share.total = 0;
+    int64_t sum = 0;
 #pragma unroll
-    for (int w = 0; w < kW; ++w) share.total += s_part[w];
-    share.total *= n_seg;
-    share.n_ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (share.total + kUnitsPerCta - 1) / kUnitsPerCta));
-    int4* desc = reinterpret_cast<int4*>(a.ws + static_cast<size_t>(gridDim.x) * 2 * kPiece);
-    if (tid == 0) desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
-    if (blockIdx.x >= share.n_ctas) return;
-    first = blockIdx.x * share.total / share.n_ctas;
-    last = (blockIdx.x + 1) * share.total / share.n_ctas;
-    // prefix sums over the sequences, kT at a time, until one passes `first`
-    __syncthreads();
+    for (int w = 0; w < kW; ++w) {
+      if (w == warp) upto += sum;
+      sum += s_part[w];
+    }
+    return sum;
+  };
+  Share share;
+  share.total = 0;
+  for (int i0 = 0; i0 < a.batch; i0 += kT) {
+    share.total += scan(i0);
+    if (blockIdx.x == 0 && i0 + tid < a.batch && (len < 0 || len > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
+  }
+  share.n_ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (share.total + kUnitsPerCta - 1) / kUnitsPerCta));
+  if (tid == 0) desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  if (blockIdx.x >= share.n_ctas) return;
+  const int64_t first = blockIdx.x * share.total / share.n_ctas;
+  const int64_t here = (blockIdx.x + 1) * share.total / share.n_ctas - first;
+  {
+    const int64_t begin_last = first + here * (kW - 1) / kW;
     int64_t before = 0;
     for (int i0 = 0; i0 < a.batch; i0 += kT) {
-      const int i = i0 + tid;
-      const int64_t units = i < a.batch ? static_cast<int64_t>(extent_of(a, i).units) * n_seg : 0;
-      int64_t upto = units;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-      }
-      if (lane == 31) s_part[warp] = upto;
-      __syncthreads();
-      int64_t total = before;
+      const int64_t sum = a.batch > kT ? scan(i0) : share.total;
 #pragma unroll
       for (int w = 0; w < kW; ++w) {
-        if (w == warp) upto += total;
-        total += s_part[w];
+        const int64_t x = first + here * w / kW - before;
+        if (upto - units <= x && x < upto) {
+          s_seq[w] = i0 + tid;
+          s_len[w] = len;
+          s_before[w] = before + upto - units;
+        }
       }
-      if (units > 0 && upto > first && upto - units <= first) {
-        s_seq = i;
-        s_before = upto - units;
-      }
-      __syncthreads();
-      before = total;
-      if (before > first) break;
+      before += sum;
+      if (before > begin_last) break;
     }
-    b = s_seq;
-    seq_start = s_before;
+    if (tid < 2 * kW) s_of[tid / 2][tid % 2].b = -1;
+    __syncthreads();
   }
+  int64_t x = first + here * warp / kW;              // the unit that is summed, among all
+  const int64_t x_end = first + here * (warp + 1) / kW;
 
-  int64_t at = first;
-  Extent ext = extent_of(a, b);
-  while (at < last) {
-    if (at >= seq_start + static_cast<int64_t>(ext.units) * n_seg) {
-      seq_start += static_cast<int64_t>(ext.units) * n_seg;
-      ext = extent_of(a, ++b);
+  // ---- the units ahead
+  Unit ahead;                                        // the next unit whose page ids are fetched
+  ahead.b = s_seq[warp];
+  ahead.ext = extent_of(a, s_len[warp]);
+  ahead.seg = static_cast<int>((x - s_before[warp]) / ahead.ext.units);
+  ahead.u = static_cast<int>((x - s_before[warp]) % ahead.ext.units);
+  int len_next = ahead.b + 1 < a.batch ? __ldg(a.lens + ahead.b + 1) : 0;
+  int64_t left = x_end - x;                          // units from `ahead` on
+  auto fetch = [&]() {
+    Unit n = ahead;
+    if (left <= 0) {                                 // past the share: nothing of it is live
+      n.ext.n = 0;
+      n.t = 0;
+      return n;
     }
-    const int seg = static_cast<int>((at - seq_start) / ext.units);
-    const int64_t seg_start = seq_start + static_cast<int64_t>(seg) * ext.units;
-    const int u0 = static_cast<int>(at - seg_start);
-    const int u1 = static_cast<int>(min(static_cast<int64_t>(ext.units), last - seg_start));
-    const int h = seg / seg_blocks, head0 = h * a.group + (seg % seg_blocks) * kSegHeads;
+    n.t = (ahead.ext.lo / kUnit + ahead.u) * kUnit;
+    if (n.t < n.ext.n) {
+      const int32_t* row = p.table + static_cast<int64_t>(n.b) * p.table_stride;
+      n.id[0] = __ldg(row + (n.t >> p.page_shift));
+      n.id[1] = p.page_shift > 3 ? n.id[0] : n.t + 8 < n.ext.n ? __ldg(row + ((n.t + 8) >> p.page_shift)) : -1;
+    }
+    if (--left > 0 && ++ahead.u == ahead.ext.units) {
+      ahead.u = 0;
+      if (++ahead.seg == n_seg) {
+        ahead.seg = 0;
+        ++ahead.b;
+        ahead.ext = extent_of(a, len_next);
+        len_next = ahead.b + 1 < a.batch ? __ldg(a.lens + ahead.b + 1) : 0;
+      }
+    }
+    return n;
+  };
+  // Where half e of a unit lies: its keys at the result, its values v_off bytes on; null where nothing of it is live.
+  const int64_t v_off = (static_cast<int64_t>(p.n_kv) << p.page_shift) * (D * 2);
+  auto place = [&](const Unit& n, int e) -> const char* {
+    const int t = n.t + 8 * e;
+    if (t >= n.ext.n || t + 8 <= n.ext.lo) return nullptr;
+    if (static_cast<uint32_t>(n.id[e]) >= static_cast<uint32_t>(p.n_pages)) {
+      if (lane == 0) raise(p.err, kBadPage);
+      return nullptr;
+    }
+    return static_cast<const char*>(p.pages) +
+           (((static_cast<int64_t>(n.id[e]) * 2 * p.n_kv + n.seg / seg_blocks) << p.page_shift) +
+            (t & ((1 << p.page_shift) - 1))) * (D * 2);
+  };
+  auto load_k = [&](const Unit& n, const char* const (&half)[2], Kreg& k) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int t = n.t + 8 * e + g;
+      const bool in = half[e] && t >= n.ext.lo && t < n.ext.n;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k.r[e][j] = in ? load_once(half[e] + g * (D * 2) + 16 * t4 + 64 * j) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto load_v = [&](const Unit& n, const char* const (&half)[2], Vreg& v) {   // (a masked token's weight is 0, 0 x NaN is not)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int t = n.t + 8 * e + 2 * t4 + i;
+        const bool in = half[e] && t >= n.ext.lo && t < n.ext.n;
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+          v.r[e][i][d] = in ? load_once(half[e] + v_off + (2 * t4 + i) * (D * 2) + 16 * g + 128 * d) : make_uint4(0, 0, 0, 0);
+      }
+  };
+  uint32_t qf[4][4];                                 // B operand of the score MMAs: column g
+  float slope0 = 0.0f, slope1 = 0.0f;
+  auto load_q = [&](const Unit& n) {
+    const int h = n.seg / seg_blocks, head0 = h * a.group + (n.seg % seg_blocks) * kSegHeads;
     const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
-    const int32_t* row = p.table + static_cast<int64_t>(b) * p.table_stride;
-
-    // ---- the queries: B operand of the score MMAs, column g
-    uint32_t qf[4][4];
+    const T* q = static_cast<const T*>(a.q.x) + n.b * a.q.token_stride + (head0 + g) * a.q.head_stride + 8 * t4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      uint4 w = make_uint4(0, 0, 0, 0);
-      if (g < n_g)
-        w = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q.x) + b * a.q.token_stride +
-                                            (head0 + g) * a.q.head_stride + 32 * j + 8 * t4);
+      const uint4 w = g < n_g ? *reinterpret_cast<const uint4*>(q + 32 * j) : make_uint4(0, 0, 0, 0);
       qf[j][0] = w.x; qf[j][1] = w.y; qf[j][2] = w.z; qf[j][3] = w.w;
     }
-    float slope0 = 0.0f, slope1 = 0.0f;
     if (a.slopes) {
-      if (2 * t4 < n_g) slope0 = a.slopes[head0 + 2 * t4] * kLog2e;
-      if (2 * t4 + 1 < n_g) slope1 = a.slopes[head0 + 2 * t4 + 1] * kLog2e;
+      slope0 = 2 * t4 < n_g ? a.slopes[head0 + 2 * t4] * kLog2e : 0.0f;
+      slope1 = 2 * t4 + 1 < n_g ? a.slopes[head0 + 2 * t4 + 1] * kLog2e : 0.0f;
     }
-    float acc[8][4];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+  };
 
-    const int unit0 = ext.lo / kUnit;
-    const int64_t v_off = (static_cast<int64_t>(p.n_kv) << p.page_shift) * (D * 2);
-    auto ids_of = [&](int u, int2& id) {             // (u may be past the end: not read then)
-      const int t = (unit0 + u) * kUnit;
-      id = make_int2(-1, -1);
-      if (u < u1 && t < ext.n) {
-        id.x = __ldg(row + (t >> p.page_shift));
-        id.y = p.page_shift > 3 ? id.x : t + 8 < ext.n ? __ldg(row + ((t + 8) >> p.page_shift)) : -1;
-      }
-    };
-    auto place_of = [&](int u, const int2& id) {
-      const int t = (unit0 + u) * kUnit;
-      Place pl;
-      pl.live_lo = max(0, ext.lo - t);
-      pl.live_hi = u < u1 ? min(kUnit, ext.n - t) : 0;
+  float acc[8][4];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int one = e ? id.y : id.x;
-        const bool live = pl.live_hi > 8 * e && pl.live_lo < 8 * e + 8;
-        const bool good = static_cast<uint32_t>(one) < static_cast<uint32_t>(p.n_pages);
-        if (live && !good && lane == 0) raise(p.err, kBadPage);
-        pl.half[e] = live && good ? static_cast<const char*>(p.pages) +
-                                        (((static_cast<int64_t>(one) * 2 * p.n_kv + h) << p.page_shift) +
-                                         ((t + 8 * e) & ((1 << p.page_shift) - 1))) * (D * 2)
-                                  : nullptr;
-      }
-      return pl;
-    };
-    auto load_k = [&](const Place& pl, Kreg& k) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const bool in = pl.half[e] && 8 * e + g >= pl.live_lo && 8 * e + g < pl.live_hi;
-        const char* src = pl.half[e] + g * (D * 2) + 16 * t4;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) k.r[e][j] = in ? load_once(src + 64 * j) : make_uint4(0, 0, 0, 0);
-      }
-    };
-    auto load_v = [&](const Place& pl, Vreg& v) {    // (a masked token's weight is 0, and 0 x NaN is not)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int tok = 8 * e + 2 * t4 + i;
-          const bool in = pl.half[e] && tok >= pl.live_lo && tok < pl.live_hi;
-          const char* src = pl.half[e] + v_off + (2 * t4 + i) * (D * 2) + 16 * g;
-#pragma unroll
-          for (int d = 0; d < 2; ++d) v.r[e][i][d] = in ? load_once(src + 128 * d) : make_uint4(0, 0, 0, 0);
-        }
-    };
-
-    int u = u0 + warp;
-    int2 id, id_next;
-    ids_of(u, id);
-    ids_of(u + kW, id_next);
-    Place pl = place_of(u, id);
+  for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
+  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
+  const int64_t x_begin = x;
+  if (x < x_end) {
+    Unit cur = fetch();
+    load_q(cur);
+    Unit next = fetch();
+    const char* half[2] = {place(cur, 0), place(cur, 1)};
     Kreg k;
     Vreg v;
-    load_k(pl, k);
-    load_v(pl, v);
-    for (; u < u1; u += kW) {
+    load_k(cur, half, k);
+    load_v(cur, half, v);
+    for (; x < x_end; ++x) {
       float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         mma<T>(s, k.r[0][j].x, k.r[1][j].x, k.r[0][j].y, k.r[1][j].y, qf[j][0], qf[j][1]);
         mma<T>(s, k.r[0][j].z, k.r[1][j].z, k.r[0][j].w, k.r[1][j].w, qf[j][2], qf[j][3]);
       }
-      const Place here = pl;
-      pl = place_of(u + kW, id_next);
-      load_k(pl, k);
-      ids_of(u + 2 * kW, id_next);
+      const bool ok0 = half[0] != nullptr, ok1 = half[1] != nullptr;
+      half[0] = place(next, 0);
+      half[1] = place(next, 1);
+      load_k(next, half, k);
+      const Unit far = fetch();
       // ---- scores in units of ln 2: s[0], s[1] token g, s[2], s[3] token g + 8; queries 2 t4, 2 t4 + 1
-      const int tok = (unit0 + u) * kUnit + g;
       if (a.cap > 0.0f) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] = a.cap * kLog2e * tanhf(s[i] * a.scale / a.cap);
@@ -435,15 +452,16 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] *= a.scale * kLog2e;
       }
+      const int tok = cur.t + g;
       if (a.slopes) {
-        const float back0 = static_cast<float>(tok - (ext.n - 1)), back1 = static_cast<float>(tok + 8 - (ext.n - 1));
+        const float back0 = static_cast<float>(tok - (cur.ext.n - 1)), back1 = static_cast<float>(tok + 8 - (cur.ext.n - 1));
         s[0] = fmaf(slope0, back0, s[0]);
         s[1] = fmaf(slope1, back0, s[1]);
         s[2] = fmaf(slope0, back1, s[2]);
         s[3] = fmaf(slope1, back1, s[3]);
       }
-      if (!here.half[0] || g < here.live_lo || g >= here.live_hi) s[0] = s[1] = -INFINITY;
-      if (!here.half[1] || g + 8 < here.live_lo || g + 8 >= here.live_hi) s[2] = s[3] = -INFINITY;
+      if (!ok0 || tok < cur.ext.lo || tok >= cur.ext.n) s[0] = s[1] = -INFINITY;
+      if (!ok1 || tok + 8 < cur.ext.lo || tok + 8 >= cur.ext.n) s[2] = s[3] = -INFINITY;
       // ---- the running reference of the exponents follows the maximum only when that is 2^8 past it
       const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
       if (__any_sync(0xffffffffu, top0 > m0 + 8.0f || top1 > m1 + 8.0f)) {
@@ -490,58 +508,113 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
         for (int e = 0; e < 2; ++e)
 #pragma unroll
           for (int d = 0; d < 2; ++d) {
-            const uint32_t x = reinterpret_cast<const uint32_t*>(&v.r[e][0][d])[i / 2];
-            const uint32_t y = reinterpret_cast<const uint32_t*>(&v.r[e][1][d])[i / 2];
-            f[2 * e + d] = __byte_perm(x, y, i % 2 ? 0x7632 : 0x5410);
+            const uint32_t y0 = reinterpret_cast<const uint32_t*>(&v.r[e][0][d])[i / 2];
+            const uint32_t y1 = reinterpret_cast<const uint32_t*>(&v.r[e][1][d])[i / 2];
+            f[2 * e + d] = __byte_perm(y0, y1, i % 2 ? 0x7632 : 0x5410);
           }
 #pragma unroll
-        for (int x = 0; x < Parts<T>::kN; ++x) mma<T>(acc[i], f[0], f[1], f[2], f[3], w[0][x], w[1][x]);
+        for (int y = 0; y < Parts<T>::kN; ++y) mma<T>(acc[i], f[0], f[1], f[2], f[3], w[0][y], w[1][y]);
       }
-      load_v(pl, v);
-    }
+      load_v(next, half, v);
 
-    // ---- join the warps
+      const bool ends = cur.u == cur.ext.units - 1;
+      if (ends || x + 1 == x_end) {                  // the segment's or the share's last unit
+        if (x + 1 < x_end) load_q(next);
+        const bool begins = x - cur.u >= x_begin;
 #pragma unroll
-    for (int o = 4; o < 32; o <<= 1) {
-      l0 += __shfl_xor_sync(0xffffffffu, l0, o);
-      l1 += __shfl_xor_sync(0xffffffffu, l1, o);
-    }
-    if (g == 0) {
-      sm[warp][2 * t4] = m0;
-      sm[warp][2 * t4 + 1] = m1;
-      sl[warp][2 * t4] = l0;
-      sl[warp][2 * t4 + 1] = l1;
-    }
+        for (int o = 4; o < 32; o <<= 1) {
+          l0 += __shfl_xor_sync(0xffffffffu, l0, o);
+          l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+        }
+        l0 *= kUnshift;
+        l1 *= kUnshift;
+        const int h = cur.seg / seg_blocks, head0 = h * a.group + (cur.seg % seg_blocks) * kSegHeads;
+        const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2; ++c) {
+          const int q = 2 * t4 + c;
+          const int64_t out_row = static_cast<int64_t>(cur.b) * a.n_q + head0 + q;
+          const float m = c ? m1 : m0, l = c ? l1 : l0;
+          float f = kUnshift, fp = 0.0f, base = 0.0f, total = l;
+          if (begins && ends) {
+            const float prior = a.prior_lse && q < n_g ? a.prior_lse[out_row] * kLog2e : -INFINITY;
+            base = fmaxf(m, prior);
+            if (base == -INFINITY) base = 0.0f;
+            const float fm = exp2_of(m - base);
+            fp = exp2_of(prior - base);
+            total = fmaf(l, fm, fp);
+            f *= fm;
+          }
+          const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+          __syncwarp();                              // (the log-sum may be written over the prior's)
 #pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        float* to = &so[warp][2 * t4 + c][64 * d + 8 * g];
-        const int x = 2 * d + c;
-        *reinterpret_cast<float4*>(to) = make_float4(acc[0][x], acc[1][x], acc[2][x], acc[3][x]);
-        *reinterpret_cast<float4*>(to + 4) = make_float4(acc[4][x], acc[5][x], acc[6][x], acc[7][x]);
+          for (int d = 0; d < 2; ++d) {
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = acc[i][2 * d + c] * f;
+            if (begins && ends) {
+              if (q >= n_g) continue;
+              float* to = a.out + out_row * D + 64 * d + 8 * g;
+              const float* from = a.prior_out + out_row * D + 64 * d + 8 * g;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) o[i] = (fp > 0.0f ? fmaf(fp, from[i], o[i]) : o[i]) * inv;
+              *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+              *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            } else {
+              float* to = &s_piece[warp][begins].sum[q][64 * d + 8 * g];
+              *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
+              *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            }
+          }
+          if (g == 0) {
+            if (begins && ends) {
+              if (a.lse && q < n_g) a.lse[out_row] = base * kLn2 + logf(total);
+            } else {
+              s_piece[warp][begins].top[q] = m;
+              s_piece[warp][begins].total[q] = l;
+            }
+          }
+        }
+        if (!(begins && ends) && lane == 0)
+          s_of[warp][begins] = {cur.b, cur.seg, ends, x - cur.u + cur.ext.units - 1};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
+        m0 = m1 = -INFINITY;
+        l0 = l1 = 0.0f;
       }
-    __syncthreads();
-    const bool begins = u0 == 0, ends = u1 == ext.units;
-    float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + (begins ? 1 : 0)) * kPiece;
+      cur = next;
+      next = far;
+    }
+  }
+  __syncthreads();
+
+  // ---- join the warps' pieces, which are in the order of the units
+  const Piece* pieces = s_piece[0];
+  const PieceOf* of = s_of[0];
+  for (int i = 0; i < 2 * kW; ++i) {
+    const PieceOf one = of[i];
+    if (one.b < 0) continue;
+    int n = i;                                       // the last piece of the same segment
+    for (int j = i + 1; j < 2 * kW; ++j)
+      if (of[j].b == one.b && of[j].seg == one.seg) n = j;
+    const bool begins = i % 2, whole = begins && of[n].ends;
+    const int h = one.seg / seg_blocks, head0 = h * a.group + (one.seg % seg_blocks) * kSegHeads;
+    const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
+    float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + begins) * kPiece;
     for (int q = 0; q < n_g; ++q) {
-      const int64_t out_row = static_cast<int64_t>(b) * a.n_q + head0 + q;
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kW; ++w) top = fmaxf(top, sm[w][q]);
-      const bool whole = begins && ends;
+      const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
       const float prior = whole && a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
-      top = fmaxf(top, prior);
+      float top = prior;
+      for (int j = i; j <= n; ++j)
+        if (of[j].b >= 0) top = fmaxf(top, pieces[j].top[q]);
       const float base = top == -INFINITY ? 0.0f : top;
       float sum = 0.0f, total = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kW; ++w) {
-        const float f = exp2_of(sm[w][q] - base);
-        sum = fmaf(f, so[w][q][tid], sum);
-        total = fmaf(f, sl[w][q], total);
-      }
-      sum *= exp2f(-Parts<T>::kShift);
-      total *= exp2f(-Parts<T>::kShift);
+      for (int j = i; j <= n; ++j)
+        if (of[j].b >= 0) {
+          const float f = exp2_of(pieces[j].top[q] - base);
+          sum = fmaf(f, pieces[j].sum[q][tid], sum);
+          total = fmaf(f, pieces[j].total[q], total);
+        }
       if (whole) {
         if (prior > -INFINITY) {
           const float f = exp2_of(prior - base);
@@ -559,12 +632,8 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
         }
       }
     }
-    if (begins && !ends && tid == 0) {
-      int4* desc = reinterpret_cast<int4*>(a.ws + static_cast<size_t>(gridDim.x) * 2 * kPiece);
-      desc[blockIdx.x] = make_int4(b, seg, cta_of(share, seg_start + ext.units - 1), 0);
-    }
-    __syncthreads();
-    at = seg_start + u1;
+    if (begins && !whole && tid == 0) desc[blockIdx.x] = make_int4(one.b, one.seg, cta_of(share, one.last_unit), 0);
+    i = n;
   }
 }
 
