@@ -472,7 +472,8 @@ aatc_status_t aatc_bf16_decode_attention(const void* K, const void* V, const voi
  * read on the device, so the library cannot refuse a bad one before the launch: every kernel
  * checks each id and length that it reads, skips what lies outside the pool, and raises a bit of
  * the caller's flags (dev_flags: device int32, ORed into, may be NULL):
- *   bit 2 (4): a page id outside [0, n_pages);  bit 3 (8): a row, index or length outside the table.
+ *   bit 1 (2): a bounded wait inside a kernel timed out;  bit 2 (4): a page id outside [0, n_pages);
+ *   bit 3 (8): a row, index or length outside the table.
  * Base pointers are 16-byte aligned, and strides (in elements) of keys, values and queries are
  * multiples of 8; the 128 values of one head are contiguous.
  */

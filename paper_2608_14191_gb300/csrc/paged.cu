@@ -130,9 +130,12 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
 // in equal sequences.
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
-constexpr int kDecodeWarps = 4;
-constexpr int kDecodeCtas = 3;      // per SM
-constexpr int kUnitsPerCta = 4;     // fewer CTAs where they would get less
+constexpr int kDecodeWarps = 8;
+constexpr int kDecodeCtas = 1;      // per SM
+constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less
+constexpr int kStages = 3;          // units of a warp on their way: keys and values, 8 KB each
+constexpr int kHalf = 8 * D * 2;    // bytes of eight tokens' keys (or values) of one head
+constexpr int kStage = 4 * kHalf;   // keys of the unit's two halves, then values
 constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128], maxima [8], totals [8]
 
 // Workspace: pieces [2 n_ctas] (CTA c's share begins inside a segment: piece 2 c; ends inside one that it began:
@@ -171,11 +174,9 @@ __device__ __forceinline__ float exp2_of(float x) {            // (-inf: 0)
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint4 load_once(const char* p) {    // 16 bytes that are read once
+__device__ __forceinline__ uint4 lds_16(uint32_t p) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p));
   return v;
 }
 
@@ -231,24 +232,17 @@ __device__ __forceinline__ int cta_of(const Share& s, int64_t unit) {
   return static_cast<int>(((unit + 1) * s.n_ctas - 1) / s.total);
 }
 
-// K and V fragments of a unit.  Lane (g, t) = (lane / 4, lane % 4) holds of K the tokens g and g + 8,
-// dimensions 32 j + 8 t .. + 7 (A operand of the score MMAs: rows are tokens, the order of the
-// dimensions is free as long as the query's is the same), and of V the tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9,
-// dimensions 8 g .. + 7 and 64 + 8 g .. + 7 (A operand of the output MMAs after pairs of tokens are
-// interleaved: rows are dimensions).  Every load is of 16 bytes, whole 32-byte sectors, straight to registers.
-struct Kreg {
-  uint4 r[2][4];                    // [token half][j]
-};
-struct Vreg {
-  uint4 r[2][2][2];                 // [token half][token][dimension half]
-};
-
-// A unit on its way through a warp: where it belongs, and the ids of the pages of its two halves.
-struct Unit {
-  int b, seg, u, t;                 // sequence, segment of it, unit of the segment, first token
-  Extent ext;
-  int id[2];
-};
+// K and V fragments of a unit.  Lane (g, t) = (lane / 4, lane % 4) needs of K the token of row g of each half
+// (A operand of the score MMAs: rows are tokens; the order of the dimensions is free as long as the query's
+// is the same) and of V the tokens of rows 2 t and 2 t + 1 of each half, dimensions 8 g .. + 7 and 64 + 8 g .. + 7
+// (A operand of the output MMAs after pairs of tokens are interleaved: rows are dimensions).  A token
+// is two rows of 128 bytes in shared memory, whose 16-byte pieces the copy has permuted by the row's
+// number modulo 8 (2 (token % 4) + the row's half).  Row r of a half is token r / 2 for even r and 4 + (r / 2 ^ 1)
+// for odd r: with it the eight lanes of every quarter of a 128-bit load of keys or values touch eight
+// different pieces.
+__device__ __forceinline__ int token_of_row(int r) { return r % 2 ? 4 + (r / 2 ^ 1) : r / 2; }
+// Piece of row half j / 2 that lane t takes in step j of the keys: {0, 1, 4, 5} and those + 2.
+__device__ __forceinline__ int piece_of(int t, int j) { return (t & 1) | (t & 2) << 1 | (j & 1) << 1; }
 
 // A warp's piece of a segment that it does not have whole, in shared memory.
 struct Piece {
@@ -261,19 +255,37 @@ struct PieceOf {
   int64_t last_unit;                // of the segment, among all units
 };
 
+// Shared memory: every warp's ring of stages, which its piece of the segment that it began takes over at the end
+// of its share, then the pieces of the segments that it found begun.
+constexpr size_t kDecodeSmem = 1024 + static_cast<size_t>(kDecodeWarps) * (kStages * kStage + sizeof(Piece));
+static_assert(sizeof(Piece) <= kStages * kStage && sizeof(Piece) % 16 == 0, "a piece in the place of a ring");
+
 template <typename T>
-__global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_decode_kernel(const DecodeArgs a) {
+__global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
+    aatc_paged_decode_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap map) {
   constexpr int kW = kDecodeWarps, kT = kW * 32;
-  static_assert(kT == D, "a thread per dimension joins the warps");
   constexpr float kUnshift = 1.0f / (1 << static_cast<int>(Parts<T>::kShift));
-  __shared__ Piece s_piece[kW][2];                   // [0]: of a segment begun before the warp's share
+  extern __shared__ unsigned char dyn_smem[];
   __shared__ PieceOf s_of[kW][2];
   __shared__ int64_t s_part[kW], s_before[kW];
   __shared__ int s_seq[kW], s_len[kW];
+  __shared__ uint64_t s_full[kW][kStages];
+  __shared__ int s_abort;
   const Pool& p = a.pool;
   const int tid = threadIdx.x, warp = ptx::warp_uniform(tid / 32), lane = tid % 32, g = lane / 4, t4 = lane % 4;
   const int seg_blocks = (a.group + kSegHeads - 1) / kSegHeads, n_seg = p.n_kv * seg_blocks;
   int4* desc = reinterpret_cast<int4*>(a.ws + static_cast<size_t>(gridDim.x) * 2 * kPiece);
+  unsigned char* rings = dyn_smem + (1024 - ptx::smem_u32(dyn_smem) % 1024) % 1024;
+  unsigned char* ring = rings + warp * (kStages * kStage);
+  auto piece_at = [&](int w, int begins) {
+    return reinterpret_cast<Piece*>(begins ? rings + w * (kStages * kStage) : rings + kW * (kStages * kStage) + w * sizeof(Piece));
+  };
+  if (tid < kW * kStages) ptx::mbar_init(&s_full[0][0] + tid, 1);
+  if (tid == 0) {
+    s_abort = 0;
+    ptx::prefetch_tmap(&map);
+  }
+  ptx::fence_mbar_init();
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
 
@@ -335,81 +347,83 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
   int64_t x = first + here * warp / kW;              // the unit that is summed, among all
   const int64_t x_end = first + here * (warp + 1) / kW;
 
-  // ---- the units ahead
-  Unit ahead;                                        // the next unit whose page ids are fetched
-  ahead.b = s_seq[warp];
-  ahead.ext = extent_of(a, s_len[warp]);
-  ahead.seg = static_cast<int>((x - s_before[warp]) / ahead.ext.units);
-  ahead.u = static_cast<int>((x - s_before[warp]) % ahead.ext.units);
-  int len_next = ahead.b + 1 < a.batch ? __ldg(a.lens + ahead.b + 1) : 0;
-  int64_t left = x_end - x;                          // units from `ahead` on
-  auto fetch = [&]() {
-    Unit n = ahead;
-    if (left <= 0) {                                 // past the share: nothing of it is live
-      n.ext.n = 0;
-      n.t = 0;
-      return n;
-    }
-    n.t = (ahead.ext.lo / kUnit + ahead.u) * kUnit;
-    if (n.t < n.ext.n) {
-      const int32_t* row = p.table + static_cast<int64_t>(n.b) * p.table_stride;
-      n.id[0] = __ldg(row + (n.t >> p.page_shift));
-      n.id[1] = p.page_shift > 3 ? n.id[0] : n.t + 8 < n.ext.n ? __ldg(row + ((n.t + 8) >> p.page_shift)) : -1;
-    }
-    if (--left > 0 && ++ahead.u == ahead.ext.units) {
-      ahead.u = 0;
-      if (++ahead.seg == n_seg) {
-        ahead.seg = 0;
-        ++ahead.b;
-        ahead.ext = extent_of(a, len_next);
-        len_next = ahead.b + 1 < a.batch ? __ldg(a.lens + ahead.b + 1) : 0;
-      }
-    }
-    return n;
+  // ---- the units ahead: a walk whose next unit has its page ids on the way, and behind it the units whose keys and
+  // values are (lane 0 issues the copies)
+  struct Walk {
+    int b, seg, u;
+    Extent ext;
+    int len_next;
   };
-  // Where half e of a unit lies: its keys at the result, its values v_off bytes on; null where nothing of it is live.
-  const int64_t v_off = (static_cast<int64_t>(p.n_kv) << p.page_shift) * (D * 2);
-  auto place = [&](const Unit& n, int e) -> const char* {
-    const int t = n.t + 8 * e;
-    if (t >= n.ext.n || t + 8 <= n.ext.lo) return nullptr;
-    if (static_cast<uint32_t>(n.id[e]) >= static_cast<uint32_t>(p.n_pages)) {
-      if (lane == 0) raise(p.err, kBadPage);
-      return nullptr;
-    }
-    return static_cast<const char*>(p.pages) +
-           (((static_cast<int64_t>(n.id[e]) * 2 * p.n_kv + n.seg / seg_blocks) << p.page_shift) +
-            (t & ((1 << p.page_shift) - 1))) * (D * 2);
+  auto step = [&](Walk& w) {
+    if (++w.u < w.ext.units) return;
+    w.u = 0;
+    if (++w.seg < n_seg) return;
+    w.seg = 0;
+    ++w.b;
+    w.ext = extent_of(a, w.len_next);
+    w.len_next = w.b + 1 < a.batch ? __ldg(a.lens + w.b + 1) : 0;
   };
-  auto load_k = [&](const Unit& n, const char* const (&half)[2], Kreg& k) {
+  Walk cur;                                          // the unit that is summed
+  cur.b = s_seq[warp];
+  cur.ext = extent_of(a, s_len[warp]);
+  cur.seg = static_cast<int>((x - s_before[warp]) / cur.ext.units);
+  cur.u = static_cast<int>((x - s_before[warp]) % cur.ext.units);
+  cur.len_next = cur.b + 1 < a.batch ? __ldg(a.lens + cur.b + 1) : 0;
+  Walk ahead = cur;                                  // the unit whose page ids are in `id`
+  int64_t x_ahead = x;
+  int id[2] = {-1, -1};
+  uint32_t good = 0;                                 // two bits a stage: the half's page is in the pool
+  auto first_token = [&](const Walk& w) { return (w.ext.lo / kUnit + w.u) * kUnit; };
+  auto fetch_ids = [&]() {
+    const int t = first_token(ahead);
+    if (x_ahead >= x_end || t >= ahead.ext.n) return;
+    const int32_t* row = p.table + static_cast<int64_t>(ahead.b) * p.table_stride;
+    id[0] = __ldg(row + (t >> p.page_shift));
+    id[1] = p.page_shift > 3 ? id[0] : t + 8 < ahead.ext.n ? __ldg(row + ((t + 8) >> p.page_shift)) : -1;
+  };
+  auto issue = [&](int stage) {                      // copies of the unit `ahead`, and the step to the next
+    if (x_ahead >= x_end) return;
+    const int t = first_token(ahead), in_page = t & ((1 << p.page_shift) - 1);
+    uint32_t ok = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int t = n.t + 8 * e + g;
-      const bool in = half[e] && t >= n.ext.lo && t < n.ext.n;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) k.r[e][j] = in ? load_once(half[e] + g * (D * 2) + 16 * t4 + 64 * j) : make_uint4(0, 0, 0, 0);
+      const bool live = t + 8 * e < ahead.ext.n && t + 8 * e + 8 > ahead.ext.lo;
+      if (live && static_cast<uint32_t>(id[e]) < static_cast<uint32_t>(p.n_pages)) ok |= 1u << e;
+      else if (live && lane == 0) raise(p.err, kBadPage);
     }
-  };
-  auto load_v = [&](const Unit& n, const char* const (&half)[2], Vreg& v) {   // (a masked token's weight is 0, 0 x NaN is not)
+    good = (good & ~(3u << 2 * stage)) | ok << 2 * stage;
+    if (lane == 0) {
+      unsigned char* to = ring + stage * kStage;
+      uint64_t* bar = &s_full[warp][stage];
+      const int row = 2 * (((ahead.seg / seg_blocks) << p.page_shift) + in_page), v_row = 2 * (p.n_kv << p.page_shift);
+      if (p.page_shift > 3) {                        // a unit lies in one page: boxes of sixteen tokens
+        ptx::mbar_arrive_expect_tx(bar, ok ? kStage : 0);
+        if (ok) {
+          ptx::tma_load_3d(to, &map, bar, 0, row, id[0]);
+          ptx::tma_load_3d(to + 2 * kHalf, &map, bar, 0, row + v_row, id[0]);
+        }
+      } else {
+        ptx::mbar_arrive_expect_tx(bar, __popc(ok) * 2 * kHalf);
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int t = n.t + 8 * e + 2 * t4 + i;
-        const bool in = half[e] && t >= n.ext.lo && t < n.ext.n;
-#pragma unroll
-        for (int d = 0; d < 2; ++d)
-          v.r[e][i][d] = in ? load_once(half[e] + v_off + (2 * t4 + i) * (D * 2) + 16 * g + 128 * d) : make_uint4(0, 0, 0, 0);
+        for (int e = 0; e < 2; ++e)
+          if (ok >> e & 1) {
+            ptx::tma_load_3d(to + e * kHalf, &map, bar, 0, row, id[e]);
+            ptx::tma_load_3d(to + (2 + e) * kHalf, &map, bar, 0, row + v_row, id[e]);
+          }
       }
+    }
+    if (++x_ahead < x_end) step(ahead);
+    fetch_ids();
   };
   uint32_t qf[4][4];                                 // B operand of the score MMAs: column g
   float slope0 = 0.0f, slope1 = 0.0f;
-  auto load_q = [&](const Unit& n) {
+  auto load_q = [&](const Walk& n) {
     const int h = n.seg / seg_blocks, head0 = h * a.group + (n.seg % seg_blocks) * kSegHeads;
     const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
-    const T* q = static_cast<const T*>(a.q.x) + n.b * a.q.token_stride + (head0 + g) * a.q.head_stride + 8 * t4;
+    const T* q = static_cast<const T*>(a.q.x) + n.b * a.q.token_stride + (head0 + g) * a.q.head_stride;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint4 w = g < n_g ? *reinterpret_cast<const uint4*>(q + 32 * j) : make_uint4(0, 0, 0, 0);
+      const uint4 w = g < n_g ? *reinterpret_cast<const uint4*>(q + 64 * (j / 2) + 8 * piece_of(t4, j)) : make_uint4(0, 0, 0, 0);
       qf[j][0] = w.x; qf[j][1] = w.y; qf[j][2] = w.z; qf[j][3] = w.w;
     }
     if (a.slopes) {
@@ -423,28 +437,55 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
   for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
   float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
   const int64_t x_begin = x;
+  // this lane's pieces: keys of row g, step j (one address for j and j ^ 2 apart); values of rows 2 t4, 2 t4 + 1
+  uint32_t k_off[4], v_off[2][2];
+  {
+    const int tok = token_of_row(g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      k_off[j] = (2 * tok + j / 2) * 128 + ((piece_of(t4, j) ^ (2 * (tok & 3) + j / 2)) * 16);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const int tk = token_of_row(2 * t4 + i);
+        v_off[i][d] = 2 * kHalf + (2 * tk + d) * 128 + ((g ^ (2 * (tk & 3) + d)) * 16);
+      }
+  }
+  bool dead = false;
   if (x < x_end) {
-    Unit cur = fetch();
+    fetch_ids();
     load_q(cur);
-    Unit next = fetch();
-    const char* half[2] = {place(cur, 0), place(cur, 1)};
-    Kreg k;
-    Vreg v;
-    load_k(cur, half, k);
-    load_v(cur, half, v);
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) issue(i);
+    int stage = 0;
+    uint32_t phase = 0;
     for (; x < x_end; ++x) {
+      if (!ptx::mbar_wait_bounded(&s_full[warp][stage], phase, &s_abort)) {
+        dead = true;
+        break;
+      }
+      const uint32_t at = ptx::smem_u32(ring) + stage * kStage;
       float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        mma<T>(s, k.r[0][j].x, k.r[1][j].x, k.r[0][j].y, k.r[1][j].y, qf[j][0], qf[j][1]);
-        mma<T>(s, k.r[0][j].z, k.r[1][j].z, k.r[0][j].w, k.r[1][j].w, qf[j][2], qf[j][3]);
+        const uint4 k0 = lds_16(at + k_off[j]), k1 = lds_16(at + kHalf + k_off[j]);
+        mma<T>(s, k0.x, k1.x, k0.y, k1.y, qf[j][0], qf[j][1]);
+        mma<T>(s, k0.z, k1.z, k0.w, k1.w, qf[j][2], qf[j][3]);
       }
-      const bool ok0 = half[0] != nullptr, ok1 = half[1] != nullptr;
-      half[0] = place(next, 0);
-      half[1] = place(next, 1);
-      load_k(next, half, k);
-      const Unit far = fetch();
-      // ---- scores in units of ln 2: s[0], s[1] token g, s[2], s[3] token g + 8; queries 2 t4, 2 t4 + 1
+      uint4 v[2][2][2];                              // [token half][token][dimension half]
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int d = 0; d < 2; ++d) v[e][i][d] = lds_16(at + e * kHalf + v_off[i][d]);
+      const int t_unit = first_token(cur);
+      const uint32_t ok = good >> 2 * stage;
+      const bool edge = t_unit < cur.ext.lo || t_unit + kUnit > cur.ext.n || (ok & 3u) != 3u;
+      __syncwarp();                                  // every lane has read the stage
+      issue(stage);
+      // ---- scores in units of ln 2: s[0], s[1] row g, s[2], s[3] row 8 + g; queries 2 t4, 2 t4 + 1
       if (a.cap > 0.0f) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] = a.cap * kLog2e * tanhf(s[i] * a.scale / a.cap);
@@ -452,7 +493,7 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] *= a.scale * kLog2e;
       }
-      const int tok = cur.t + g;
+      const int tok = t_unit + token_of_row(g);
       if (a.slopes) {
         const float back0 = static_cast<float>(tok - (cur.ext.n - 1)), back1 = static_cast<float>(tok + 8 - (cur.ext.n - 1));
         s[0] = fmaf(slope0, back0, s[0]);
@@ -460,8 +501,17 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
         s[2] = fmaf(slope0, back1, s[2]);
         s[3] = fmaf(slope1, back1, s[3]);
       }
-      if (!ok0 || tok < cur.ext.lo || tok >= cur.ext.n) s[0] = s[1] = -INFINITY;
-      if (!ok1 || tok + 8 < cur.ext.lo || tok + 8 >= cur.ext.n) s[2] = s[3] = -INFINITY;
+      if (edge) {
+        if (!(ok & 1u) || tok < cur.ext.lo || tok >= cur.ext.n) s[0] = s[1] = -INFINITY;
+        if (!(ok & 2u) || tok + 8 < cur.ext.lo || tok + 8 >= cur.ext.n) s[2] = s[3] = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {              // a masked token's weight is 0, but 0 x NaN is not
+            const int t = t_unit + 8 * e + token_of_row(2 * t4 + i);
+            if (!(ok >> e & 1u) || t < cur.ext.lo || t >= cur.ext.n) v[e][i][0] = v[e][i][1] = make_uint4(0, 0, 0, 0);
+          }
+      }
       // ---- the running reference of the exponents follows the maximum only when that is 2^8 past it
       const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
       if (__any_sync(0xffffffffu, top0 > m0 + 8.0f || top1 > m1 + 8.0f)) {
@@ -508,17 +558,18 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
         for (int e = 0; e < 2; ++e)
 #pragma unroll
           for (int d = 0; d < 2; ++d) {
-            const uint32_t y0 = reinterpret_cast<const uint32_t*>(&v.r[e][0][d])[i / 2];
-            const uint32_t y1 = reinterpret_cast<const uint32_t*>(&v.r[e][1][d])[i / 2];
+            const uint32_t y0 = reinterpret_cast<const uint32_t*>(&v[e][0][d])[i / 2];
+            const uint32_t y1 = reinterpret_cast<const uint32_t*>(&v[e][1][d])[i / 2];
             f[2 * e + d] = __byte_perm(y0, y1, i % 2 ? 0x7632 : 0x5410);
           }
 #pragma unroll
         for (int y = 0; y < Parts<T>::kN; ++y) mma<T>(acc[i], f[0], f[1], f[2], f[3], w[0][y], w[1][y]);
       }
-      load_v(next, half, v);
 
       const bool ends = cur.u == cur.ext.units - 1;
       if (ends || x + 1 == x_end) {                  // the segment's or the share's last unit
+        Walk next = cur;
+        step(next);
         if (x + 1 < x_end) load_q(next);
         const bool begins = x - cur.u >= x_begin;
 #pragma unroll
@@ -561,7 +612,7 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
               *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
               *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
             } else {
-              float* to = &s_piece[warp][begins].sum[q][64 * d + 8 * g];
+              float* to = &piece_at(warp, begins)->sum[q][64 * d + 8 * g];
               *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
               *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
             }
@@ -570,8 +621,8 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
             if (begins && ends) {
               if (a.lse && q < n_g) a.lse[out_row] = base * kLn2 + logf(total);
             } else {
-              s_piece[warp][begins].top[q] = m;
-              s_piece[warp][begins].total[q] = l;
+              piece_at(warp, begins)->top[q] = m;
+              piece_at(warp, begins)->total[q] = l;
             }
           }
         }
@@ -582,15 +633,28 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
         m0 = m1 = -INFINITY;
         l0 = l1 = 0.0f;
       }
-      cur = next;
-      next = far;
+      if (x + 1 < x_end) step(cur);
+      if (++stage == kStages) {
+        stage = 0;
+        phase ^= 1;
+      }
+    }
+    if (dead) {                                      // a copy did not arrive: tell, and wait out those under way
+      if (lane == 0) raise(p.err, kTimeout);
+      for (++x; x < x_ahead; ++x) {
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1;
+        }
+        ptx::mbar_wait_bounded(&s_full[warp][stage], phase, &s_abort);
+      }
     }
   }
   __syncthreads();
 
   // ---- join the warps' pieces, which are in the order of the units
-  const Piece* pieces = s_piece[0];
   const PieceOf* of = s_of[0];
+  const int dim = tid % D;                           // a thread takes this dimension of every (kT / D)-th head
   for (int i = 0; i < 2 * kW; ++i) {
     const PieceOf one = of[i];
     if (one.b < 0) continue;
@@ -601,32 +665,33 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas) aatc_paged_dec
     const int h = one.seg / seg_blocks, head0 = h * a.group + (one.seg % seg_blocks) * kSegHeads;
     const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
     float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + begins) * kPiece;
-    for (int q = 0; q < n_g; ++q) {
+    for (int q = tid / D; q < n_g; q += kT / D) {
       const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
       const float prior = whole && a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
       float top = prior;
       for (int j = i; j <= n; ++j)
-        if (of[j].b >= 0) top = fmaxf(top, pieces[j].top[q]);
+        if (of[j].b >= 0) top = fmaxf(top, piece_at(j / 2, j % 2)->top[q]);
       const float base = top == -INFINITY ? 0.0f : top;
       float sum = 0.0f, total = 0.0f;
       for (int j = i; j <= n; ++j)
         if (of[j].b >= 0) {
-          const float f = exp2_of(pieces[j].top[q] - base);
-          sum = fmaf(f, pieces[j].sum[q][tid], sum);
-          total = fmaf(f, pieces[j].total[q], total);
+          const Piece* one_of = piece_at(j / 2, j % 2);
+          const float f = exp2_of(one_of->top[q] - base);
+          sum = fmaf(f, one_of->sum[q][dim], sum);
+          total = fmaf(f, one_of->total[q], total);
         }
       if (whole) {
         if (prior > -INFINITY) {
           const float f = exp2_of(prior - base);
-          sum = fmaf(f, a.prior_out[out_row * D + tid], sum);
+          sum = fmaf(f, a.prior_out[out_row * D + dim], sum);
           total += f;
         }
-        a.out[out_row * D + tid] = total == 0.0f ? 0.0f : sum / total;
-        __syncthreads();                             // (the log-sum may be written over the prior's)
-        if (a.lse && tid == 0) a.lse[out_row] = base * kLn2 + logf(total);
+        a.out[out_row * D + dim] = total == 0.0f ? 0.0f : sum / total;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + tid / D), "n"(D) : "memory");   // (the log-sum may replace the prior's)
+        if (a.lse && dim == 0) a.lse[out_row] = base * kLn2 + logf(total);
       } else {
-        piece[q * D + tid] = sum;
-        if (tid == 0) {
+        piece[q * D + dim] = sum;
+        if (dim == 0) {
           piece[kSegHeads * D + q] = top;
           piece[kSegHeads * D + kSegHeads + q] = total;
         }
@@ -748,7 +813,15 @@ size_t decode_workspace(int num_sms) {
 cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
   const int ctas = std::max(1, a.num_sms) * kDecodeCtas;
   const auto kernel = dtype == AATC_BF16 ? aatc_paged_decode_kernel<__nv_bfloat16> : aatc_paged_decode_kernel<__half>;
-  const cudaError_t e = launch_pdl(kernel, dim3(ctas), dim3(kDecodeWarps * 32), 0, st, a);
+  // pages as rows of 128 bytes, two a token; a box is a unit's tokens in a page
+  CUtensorMap map;
+  const uint64_t rows = static_cast<uint64_t>(4) * a.pool.n_kv << a.pool.page_shift;
+  cudaError_t e = make_tensor_map_3d(&map, a.pool.pages, D / 2, rows, a.pool.n_pages, D, rows * D, D / 2,
+                                     2 * std::min(kUnit, 1 << a.pool.page_shift));
+  if (e != cudaSuccess) return e;
+  e = ensure_smem_optin(reinterpret_cast<const void*>(kernel), kDecodeSmem);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(kernel, dim3(ctas), dim3(kDecodeWarps * 32), kDecodeSmem, st, a, map);
   if (e != cudaSuccess) return e;
   return launch_pdl(aatc_paged_join_kernel, dim3(ctas, std::min(a.group, kSegHeads)), dim3(kJoinWarps * 32), 0, st, a, ctas);
 }

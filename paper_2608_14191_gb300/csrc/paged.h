@@ -13,6 +13,7 @@ namespace aatc {
 namespace paged {
 
 // Device flags of the paged calls (include/aatc.h).
+constexpr int kTimeout = 2;
 constexpr int kBadPage = 4;
 constexpr int kBadRow = 8;
 

@@ -128,8 +128,8 @@ class Pages:
         return torch.empty(max(4, self.decode_workspace_bytes(n_q_heads) // 4), dtype=_F32T, device=self.device)
 
     def device_error(self, clear: bool = False) -> int:
-        """Flags that kernels raised (4: a page id outside the pool, 8: a row, index or length outside the
-        table).  Synchronizes."""
+        """Flags that kernels raised (2: a bounded wait timed out, 4: a page id outside the pool, 8: a row,
+        index or length outside the table).  Synchronizes."""
         f = int(self.flags.item())
         if clear:
             self.flags.zero_()
