@@ -121,21 +121,24 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
 // ---------------------------------------------------------------- decode attention
 // The work of a call is its units of 16 tokens: those of sequence 0's kv-head 0, then kv-head 1, ...,
 // then sequence 1's, a (sequence, kv-head) being a segment.  CTA c of n takes the units
-// [c U / n, (c + 1) U / n) of all U and each of its warps a quarter of those, so every warp has the same
-// share whatever the lengths.  A segment that lies inside a warp's share is finished by the warp, the pieces of one
-// that lies in several warps are joined in shared memory, and those of one in several CTAs
+// [c U / n, (c + 1) U / n) of all U and each of its consumer warps an eighth of those, so every warp has the
+// same share whatever the lengths.  A segment that lies inside a warp's share is finished by the warp, the
+// pieces of one that lies in several warps are joined in shared memory, and those of one in several CTAs
 // through the workspace by the second launch.  (Query heads beyond eight of a kv-head are further segments over
-// the same tokens.)  A warp's loads run ahead of its sums across the segments of its share: with
-// shares by CTA and a barrier per segment, 61 sequences of 62 to 4001 tokens took twice as long as as many tokens
-// in equal sequences.
+// the same tokens.)  One more warp brings the units: a lane of it walks each consumer's share, across
+// the segments, and keeps a ring of units under way by TMA.  So the consumers execute little more than the
+// matrix instructions and the softmax: with the walk in every warp a unit took 530 instructions, and eight
+// warps an SM were held up by issue latency before the memory was.
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
-constexpr int kDecodeWarps = 8;
-constexpr int kDecodeCtas = 1;      // per SM
+constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM
+constexpr int kProducers = 4;       // producer warps
+constexpr int kServes = kConsumers / kProducers;
+constexpr int kDecodeThreads = (kConsumers + kProducers) * 32;
 constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less
-constexpr int kStages = 3;          // units of a warp on their way: keys and values, 8 KB each
-constexpr int kHalf = 8 * D * 2;    // bytes of eight tokens' keys (or values) of one head
-constexpr int kStage = 4 * kHalf;   // keys of the unit's two halves, then values
+constexpr int kStages = 3;          // units of a consumer on their way: keys and values, 8 KB each
+constexpr int kRow = 128;           // bytes of half a token's key or value: a row in shared memory
+constexpr int kStage = kUnit * 4 * kRow;      // keys, then values
 constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128], maxima [8], totals [8]
 
 // Workspace: pieces [2 n_ctas] (CTA c's share begins inside a segment: piece 2 c; ends inside one that it began:
@@ -147,23 +150,34 @@ struct Share {
 };
 
 template <typename T>
-__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                    uint32_t b1);
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
 template <>
-__device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                                   uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <>
-__device__ __forceinline__ void mma<__half>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                            uint32_t b1) {
+__device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Four 8 x 8 matrices of 16-bit values, lane l giving the address of row l % 8 of matrix l / 8; lane
+// (g, t) = (l / 4, l % 4) gets values 2 t, 2 t + 1 of row g, of the transposed matrices in the second form.
+__device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of an 8 x 8 matrix of 16-bit values over the warp
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -174,10 +188,12 @@ __device__ __forceinline__ float exp2_of(float x) {            // (-inf: 0)
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint4 lds_16(uint32_t p) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p));
-  return v;
+// tanh x = 1 - 2 / (e^(2 x) + 1), and where that cancels its Taylor series: either within 4e-7 of its value
+__device__ __forceinline__ float tanh_of(float x) {
+  const float a = fabsf(x), x2 = x * x;
+  const float big = 1.0f - __fdividef(2.0f, exp2_of(2.0f * kLog2e * a) + 1.0f);
+  const float small = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+  return a < 0.25f ? x * small : copysignf(a > 20.0f ? 1.0f : big, x);
 }
 
 // A weight p as a sum of 16-bit values, so that products with 16-bit values on the tensor cores lose
@@ -232,17 +248,12 @@ __device__ __forceinline__ int cta_of(const Share& s, int64_t unit) {
   return static_cast<int>(((unit + 1) * s.n_ctas - 1) / s.total);
 }
 
-// K and V fragments of a unit.  Lane (g, t) = (lane / 4, lane % 4) needs of K the token of row g of each half
-// (A operand of the score MMAs: rows are tokens; the order of the dimensions is free as long as the query's
-// is the same) and of V the tokens of rows 2 t and 2 t + 1 of each half, dimensions 8 g .. + 7 and 64 + 8 g .. + 7
-// (A operand of the output MMAs after pairs of tokens are interleaved: rows are dimensions).  A token
-// is two rows of 128 bytes in shared memory, whose 16-byte pieces the copy has permuted by the row's
-// number modulo 8 (2 (token % 4) + the row's half).  Row r of a half is token r / 2 for even r and 4 + (r / 2 ^ 1)
-// for odd r: with it the eight lanes of every quarter of a 128-bit load of keys or values touch eight
-// different pieces.
-__device__ __forceinline__ int token_of_row(int r) { return r % 2 ? 4 + (r / 2 ^ 1) : r / 2; }
-// Piece of row half j / 2 that lane t takes in step j of the keys: {0, 1, 4, 5} and those + 2.
-__device__ __forceinline__ int piece_of(int t, int j) { return (t & 1) | (t & 2) << 1 | (j & 1) << 1; }
+// What a consumer learns of a unit: its first token, the live ones [lo, n) of its sequence, whether the pages of
+// its halves are in the pool (bits 0, 1 of `ok`), and where it belongs.
+struct __align__(16) Unit {
+  int t, lo, n, ok;
+  int b, seg, u, units;
+};
 
 // A warp's piece of a segment that it does not have whole, in shared memory.
 struct Piece {
@@ -255,32 +266,41 @@ struct PieceOf {
   int64_t last_unit;                // of the segment, among all units
 };
 
-// Shared memory: every warp's ring of stages, which its piece of the segment that it began takes over at the end
-// of its share, then the pieces of the segments that it found begun.
-constexpr size_t kDecodeSmem = 1024 + static_cast<size_t>(kDecodeWarps) * (kStages * kStage + sizeof(Piece));
+// Shared memory: every consumer's ring of stages, which its piece of the segment that it began takes over at the
+// end of its share, then the pieces of the segments that it found begun.
+constexpr size_t kDecodeSmem = static_cast<size_t>(kConsumers) * (kStages * kStage + sizeof(Piece));
 static_assert(sizeof(Piece) <= kStages * kStage && sizeof(Piece) % 16 == 0, "a piece in the place of a ring");
 
+// What one lane of the producer does for its consumer: the walk over the share's units.
+struct Walk {
+  int b, seg, u, len_next;
+  Extent ext;
+};
+
 template <typename T>
-__global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
+__global__ void __launch_bounds__(kDecodeThreads, 1)
     aatc_paged_decode_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap map) {
-  constexpr int kW = kDecodeWarps, kT = kW * 32;
+  constexpr int kW = kConsumers, kT = kDecodeThreads;
   constexpr float kUnshift = 1.0f / (1 << static_cast<int>(Parts<T>::kShift));
-  extern __shared__ unsigned char dyn_smem[];
+  extern __shared__ __align__(1024) unsigned char rings[];   // (the copies' permutation goes by 1024-byte blocks)
   __shared__ PieceOf s_of[kW][2];
-  __shared__ int64_t s_part[kW], s_before[kW];
+  __shared__ Unit s_unit[kW][kStages];
+  __shared__ int64_t s_part[kW + kProducers], s_before[kW];
   __shared__ int s_seq[kW], s_len[kW];
-  __shared__ uint64_t s_full[kW][kStages];
+  __shared__ uint64_t s_full[kW][kStages], s_free[kW][kStages];
   __shared__ int s_abort;
   const Pool& p = a.pool;
-  const int tid = threadIdx.x, warp = ptx::warp_uniform(tid / 32), lane = tid % 32, g = lane / 4, t4 = lane % 4;
+  const int tid = threadIdx.x, warp = ptx::warp_uniform(tid / 32), lane = tid % 32;
   const int seg_blocks = (a.group + kSegHeads - 1) / kSegHeads, n_seg = p.n_kv * seg_blocks;
   int4* desc = reinterpret_cast<int4*>(a.ws + static_cast<size_t>(gridDim.x) * 2 * kPiece);
-  unsigned char* rings = dyn_smem + (1024 - ptx::smem_u32(dyn_smem) % 1024) % 1024;
-  unsigned char* ring = rings + warp * (kStages * kStage);
   auto piece_at = [&](int w, int begins) {
     return reinterpret_cast<Piece*>(begins ? rings + w * (kStages * kStage) : rings + kW * (kStages * kStage) + w * sizeof(Piece));
   };
-  if (tid < kW * kStages) ptx::mbar_init(&s_full[0][0] + tid, 1);
+  if (tid < kW * kStages) {
+    ptx::mbar_init(&s_full[0][0] + tid, 1);
+    ptx::mbar_init(&s_free[0][0] + tid, 1);
+  }
+  if (tid < 2 * kW) s_of[tid / 2][tid % 2].b = -1;
   if (tid == 0) {
     s_abort = 0;
     ptx::prefetch_tmap(&map);
@@ -299,15 +319,15 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
     upto = units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += x;
+      const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
     }
     __syncthreads();                                 // (the last chunk's sums have been read)
     if (lane == 31) s_part[warp] = upto;
     __syncthreads();
     int64_t sum = 0;
 #pragma unroll
-    for (int w = 0; w < kW; ++w) {
+    for (int w = 0; w < kW + kProducers; ++w) {
       if (w == warp) upto += sum;
       sum += s_part[w];
     }
@@ -331,8 +351,8 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
       const int64_t sum = a.batch > kT ? scan(i0) : share.total;
 #pragma unroll
       for (int w = 0; w < kW; ++w) {
-        const int64_t x = first + here * w / kW - before;
-        if (upto - units <= x && x < upto) {
+        const int64_t y = first + here * w / kW - before;
+        if (upto - units <= y && y < upto) {
           s_seq[w] = i0 + tid;
           s_len[w] = len;
           s_before[w] = before + upto - units;
@@ -341,179 +361,189 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
       before += sum;
       if (before > begin_last) break;
     }
-    if (tid < 2 * kW) s_of[tid / 2][tid % 2].b = -1;
     __syncthreads();
   }
-  int64_t x = first + here * warp / kW;              // the unit that is summed, among all
-  const int64_t x_end = first + here * (warp + 1) / kW;
 
-  // ---- the units ahead: a walk whose next unit has its page ids on the way, and behind it the units whose keys and
-  // values are (lane 0 issues the copies)
-  struct Walk {
-    int b, seg, u;
-    Extent ext;
-    int len_next;
-  };
-  auto step = [&](Walk& w) {
-    if (++w.u < w.ext.units) return;
-    w.u = 0;
-    if (++w.seg < n_seg) return;
-    w.seg = 0;
-    ++w.b;
-    w.ext = extent_of(a, w.len_next);
-    w.len_next = w.b + 1 < a.batch ? __ldg(a.lens + w.b + 1) : 0;
-  };
-  Walk cur;                                          // the unit that is summed
-  cur.b = s_seq[warp];
-  cur.ext = extent_of(a, s_len[warp]);
-  cur.seg = static_cast<int>((x - s_before[warp]) / cur.ext.units);
-  cur.u = static_cast<int>((x - s_before[warp]) % cur.ext.units);
-  cur.len_next = cur.b + 1 < a.batch ? __ldg(a.lens + cur.b + 1) : 0;
-  Walk ahead = cur;                                  // the unit whose page ids are in `id`
-  int64_t x_ahead = x;
-  int id[2] = {-1, -1};
-  uint32_t good = 0;                                 // two bits a stage: the half's page is in the pool
-  auto first_token = [&](const Walk& w) { return (w.ext.lo / kUnit + w.u) * kUnit; };
-  auto fetch_ids = [&]() {
-    const int t = first_token(ahead);
-    if (x_ahead >= x_end || t >= ahead.ext.n) return;
-    const int32_t* row = p.table + static_cast<int64_t>(ahead.b) * p.table_stride;
-    id[0] = __ldg(row + (t >> p.page_shift));
-    id[1] = p.page_shift > 3 ? id[0] : t + 8 < ahead.ext.n ? __ldg(row + ((t + 8) >> p.page_shift)) : -1;
-  };
-  auto issue = [&](int stage) {                      // copies of the unit `ahead`, and the step to the next
-    if (x_ahead >= x_end) return;
-    const int t = first_token(ahead), in_page = t & ((1 << p.page_shift) - 1);
-    uint32_t ok = 0;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const bool live = t + 8 * e < ahead.ext.n && t + 8 * e + 8 > ahead.ext.lo;
-      if (live && static_cast<uint32_t>(id[e]) < static_cast<uint32_t>(p.n_pages)) ok |= 1u << e;
-      else if (live && lane == 0) raise(p.err, kBadPage);
-    }
-    good = (good & ~(3u << 2 * stage)) | ok << 2 * stage;
-    if (lane == 0) {
-      unsigned char* to = ring + stage * kStage;
-      uint64_t* bar = &s_full[warp][stage];
-      const int row = 2 * (((ahead.seg / seg_blocks) << p.page_shift) + in_page), v_row = 2 * (p.n_kv << p.page_shift);
-      if (p.page_shift > 3) {                        // a unit lies in one page: boxes of sixteen tokens
-        ptx::mbar_arrive_expect_tx(bar, ok ? kStage : 0);
-        if (ok) {
-          ptx::tma_load_3d(to, &map, bar, 0, row, id[0]);
-          ptx::tma_load_3d(to + 2 * kHalf, &map, bar, 0, row + v_row, id[0]);
+  // second eight tokens and second halves of the heads in a stage
+  const int e_off = p.page_shift > 3 ? 8 * kRow : 16 * kRow, h_off = p.page_shift > 3 ? 16 * kRow : 8 * kRow;
+  if (warp >= kW) {
+    // ---- a producer: each of its first lanes serves a consumer
+    const bool serves = lane < kServes;
+    const int w = (warp - kW) * kServes + (serves ? lane : 0);
+    int64_t x = first + here * w / kW;
+    const int64_t x_end = serves ? first + here * (w + 1) / kW : x;
+    Walk at;
+    at.b = s_seq[w];
+    at.ext = extent_of(a, s_len[w]);
+    at.seg = static_cast<int>((x - s_before[w]) / at.ext.units);
+    at.u = static_cast<int>((x - s_before[w]) % at.ext.units);
+    at.len_next = at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
+    int id0 = -1, id1 = -1;                          // pages of the unit's halves
+    auto fetch_ids = [&]() {
+      const int t = (at.ext.lo / kUnit + at.u) * kUnit;
+      if (x >= x_end || t >= at.ext.n) return;
+      const int32_t* row = p.table + static_cast<int64_t>(at.b) * p.table_stride;
+      id0 = __ldg(row + (t >> p.page_shift));
+      id1 = p.page_shift > 3 ? id0 : t + 8 < at.ext.n ? __ldg(row + ((t + 8) >> p.page_shift)) : -1;
+    };
+    fetch_ids();
+    int stage = 0, round = 0;
+    uint64_t idle_since = 0;
+    for (;;) {
+      const bool work = x < x_end;
+      if (!__any_sync(0xffffffffu, work)) break;
+      const bool can = work && (round == 0 || ptx::mbar_test_wait(&s_free[w][stage], (round - 1) & 1));
+      if (can) {
+        const int t = (at.ext.lo / kUnit + at.u) * kUnit;
+        bool ok0 = t < at.ext.n && t + 8 > at.ext.lo, ok1 = t + 8 < at.ext.n;      // live (a unit has t + 16 > lo)
+        if ((ok0 && static_cast<uint32_t>(id0) >= static_cast<uint32_t>(p.n_pages)) ||
+            (ok1 && static_cast<uint32_t>(id1) >= static_cast<uint32_t>(p.n_pages))) {
+          raise(p.err, kBadPage);
+          ok0 = ok0 && static_cast<uint32_t>(id0) < static_cast<uint32_t>(p.n_pages);
+          ok1 = ok1 && static_cast<uint32_t>(id1) < static_cast<uint32_t>(p.n_pages);
         }
-      } else {
-        ptx::mbar_arrive_expect_tx(bar, __popc(ok) * 2 * kHalf);
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (ok >> e & 1) {
-            ptx::tma_load_3d(to + e * kHalf, &map, bar, 0, row, id[e]);
-            ptx::tma_load_3d(to + (2 + e) * kHalf, &map, bar, 0, row + v_row, id[e]);
+        Unit* un = &s_unit[w][stage];
+        *reinterpret_cast<int4*>(&un->t) = make_int4(t, at.ext.lo, at.ext.n, (ok0 ? 1 : 0) | (ok1 ? 2 : 0));
+        *reinterpret_cast<int4*>(&un->b) = make_int4(at.b, at.seg, at.u, at.ext.units);
+        unsigned char* to = rings + (w * kStages + stage) * kStage;
+        uint64_t* bar = &s_full[w][stage];
+        const int row = ((at.seg / seg_blocks) << p.page_shift) + (t & ((1 << p.page_shift) - 1)), v_row = p.n_kv << p.page_shift;
+        // a box is one half of the heads' values: of sixteen tokens where a unit lies in one page, else of eight
+        auto copy = [&](unsigned char* dst, int id) {
+          ptx::tma_load_3d(dst, &map, bar, 0, row, id);
+          ptx::tma_load_3d(dst + h_off, &map, bar, D / 2, row, id);
+          ptx::tma_load_3d(dst + kStage / 2, &map, bar, 0, row + v_row, id);
+          ptx::tma_load_3d(dst + kStage / 2 + h_off, &map, bar, D / 2, row + v_row, id);
+        };
+        if (p.page_shift > 3) {
+          ptx::mbar_arrive_expect_tx(bar, ok0 || ok1 ? kStage : 0);
+          if (ok0 || ok1) copy(to, id0);
+        } else {
+          ptx::mbar_arrive_expect_tx(bar, (ok0 ? kStage / 2 : 0) + (ok1 ? kStage / 2 : 0));
+          if (ok0) copy(to, id0);
+          if (ok1) copy(to + e_off, id1);
+        }
+        if (++x < x_end && ++at.u == at.ext.units) {
+          at.u = 0;
+          if (++at.seg == n_seg) {
+            at.seg = 0;
+            ++at.b;
+            at.ext = extent_of(a, at.len_next);
+            at.len_next = at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
           }
+        }
+        fetch_ids();
+        if (++stage == kStages) {
+          stage = 0;
+          ++round;
+        }
+        idle_since = 0;
+      }
+      if (!__any_sync(0xffffffffu, can)) {           // (a consumer that stopped, stops this too)
+        if (*reinterpret_cast<volatile int*>(&s_abort)) break;
+        const uint64_t now = ptx::globaltimer_ns();
+        if (idle_since == 0) idle_since = now;
+        if (__any_sync(0xffffffffu, now - idle_since > 2000000000ull)) break;
       }
     }
-    if (++x_ahead < x_end) step(ahead);
-    fetch_ids();
-  };
-  uint32_t qf[4][4];                                 // B operand of the score MMAs: column g
-  float slope0 = 0.0f, slope1 = 0.0f;
-  auto load_q = [&](const Walk& n) {
-    const int h = n.seg / seg_blocks, head0 = h * a.group + (n.seg % seg_blocks) * kSegHeads;
-    const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
-    const T* q = static_cast<const T*>(a.q.x) + n.b * a.q.token_stride + (head0 + g) * a.q.head_stride;
+  } else {
+    // ---- a consumer
+    const int g = lane / 4, t4 = lane % 4;
+    int64_t x = first + here * warp / kW;
+    const int64_t x_begin = x, x_end = first + here * (warp + 1) / kW;
+    unsigned char* ring = rings + warp * (kStages * kStage);
+    // Rows of 128 bytes: [half of the head's values][token] of a page's eight or sixteen tokens, their 16-byte pieces permuted
+    // by the row's number modulo 8.  Keys: matrices (tokens 0 .. 7, 8 .. 15) x (piece, next piece), the A operand of
+    // a score MMA, whose rows are tokens; values: (piece, next) x (tokens 0 .. 7, 8 .. 15), transposed the A
+    // operand of an output MMA, whose rows are dimensions.
+    const uint32_t k_at = (lane / 8 % 2) * e_off + lane % 8 * kRow + ((lane / 16) ^ lane % 8) * 16;
+    const uint32_t v_at = kStage / 2 + (lane / 16) * e_off + lane % 8 * kRow + ((lane / 8 % 2) ^ lane % 8) * 16;
+    const float unit_scale = a.scale * kLog2e, cap_in = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap_out = a.cap * kLog2e;
+    const bool plain = a.cap <= 0.0f && !a.slopes;
+    uint32_t qf[8][2];                               // B operand of the score MMAs: column g
+    float slope0 = 0.0f, slope1 = 0.0f;
+    float acc[8][4];                                 // dimensions 16 i + g, 16 i + 8 + g; queries 2 t4, 2 t4 + 1
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint4 w = g < n_g ? *reinterpret_cast<const uint4*>(q + 64 * (j / 2) + 8 * piece_of(t4, j)) : make_uint4(0, 0, 0, 0);
-      qf[j][0] = w.x; qf[j][1] = w.y; qf[j][2] = w.z; qf[j][3] = w.w;
-    }
-    if (a.slopes) {
-      slope0 = 2 * t4 < n_g ? a.slopes[head0 + 2 * t4] * kLog2e : 0.0f;
-      slope1 = 2 * t4 + 1 < n_g ? a.slopes[head0 + 2 * t4 + 1] * kLog2e : 0.0f;
-    }
-  };
-
-  float acc[8][4];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
-  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-  const int64_t x_begin = x;
-  // this lane's pieces: keys of row g, step j (one address for j and j ^ 2 apart); values of rows 2 t4, 2 t4 + 1
-  uint32_t k_off[4], v_off[2][2];
-  {
-    const int tok = token_of_row(g);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      k_off[j] = (2 * tok + j / 2) * 128 + ((piece_of(t4, j) ^ (2 * (tok & 3) + j / 2)) * 16);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        const int tk = token_of_row(2 * t4 + i);
-        v_off[i][d] = 2 * kHalf + (2 * tk + d) * 128 + ((g ^ (2 * (tk & 3) + d)) * 16);
-      }
-  }
-  bool dead = false;
-  if (x < x_end) {
-    fetch_ids();
-    load_q(cur);
-#pragma unroll
-    for (int i = 0; i < kStages; ++i) issue(i);
+    for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
     int stage = 0;
     uint32_t phase = 0;
+    bool fresh = true;                               // the next unit is of another segment
     for (; x < x_end; ++x) {
       if (!ptx::mbar_wait_bounded(&s_full[warp][stage], phase, &s_abort)) {
-        dead = true;
+        if (lane == 0) {                             // a copy did not arrive: tell, and stop the others
+          raise(p.err, kTimeout);
+          *reinterpret_cast<volatile int*>(&s_abort) = 1;
+        }
         break;
       }
-      const uint32_t at = ptx::smem_u32(ring) + stage * kStage;
-      float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      const int4 ua = *reinterpret_cast<const int4*>(&s_unit[warp][stage].t);      // t, lo, n, ok
+      const int4 ub = *reinterpret_cast<const int4*>(&s_unit[warp][stage].b);      // b, seg, u, units
+      const int h = ub.y / seg_blocks, head0 = h * a.group + (ub.y % seg_blocks) * kSegHeads;
+      const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
+      if (fresh) {
+        const T* q = static_cast<const T*>(a.q.x) + ub.x * a.q.token_stride + (head0 + g) * a.q.head_stride + 2 * t4;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          qf[j][0] = g < n_g ? *reinterpret_cast<const uint32_t*>(q + 16 * j) : 0u;
+          qf[j][1] = g < n_g ? *reinterpret_cast<const uint32_t*>(q + 16 * j + 8) : 0u;
+        }
+        if (a.slopes) {
+          slope0 = 2 * t4 < n_g ? a.slopes[head0 + 2 * t4] * kLog2e : 0.0f;
+          slope1 = 2 * t4 + 1 < n_g ? a.slopes[head0 + 2 * t4 + 1] * kLog2e : 0.0f;
+        }
+        fresh = false;
+      }
+      const uint32_t base = ptx::smem_u32(ring) + stage * kStage;
+      const bool edge = ua.x < ua.y || ua.x + kUnit > ua.z || ua.w != 3;
+      if (edge) {                                    // values of masked tokens: their weight is 0, but 0 x NaN is not
+        for (int i = lane; i < kUnit * 2 * kRow / 16; i += 32) {
+          const int tok = i / 8 % 16, e = tok / 8;
+          if (!(ua.w >> e & 1) || ua.x + tok < ua.y || ua.x + tok >= ua.z)
+            *reinterpret_cast<uint4*>(ring + stage * kStage + kStage / 2 + e * e_off + i / 128 * h_off + tok % 8 * kRow + i % 8 * 16) =
+                make_uint4(0, 0, 0, 0);
+        }
+        ptx::fence_proxy_async_smem();               // (the next copy to the stage comes after)
+        __syncwarp();
+      }
+      float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s2[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint4 k0 = lds_16(at + k_off[j]), k1 = lds_16(at + kHalf + k_off[j]);
-        mma<T>(s, k0.x, k1.x, k0.y, k1.y, qf[j][0], qf[j][1]);
-        mma<T>(s, k0.z, k1.z, k0.w, k1.w, qf[j][2], qf[j][3]);
+        uint32_t k0[4], k1[4];
+        ldsm(k0, base + (k_at ^ 32 * j));
+        ldsm(k1, base + h_off + (k_at ^ 32 * j));
+        mma<T>(s, k0, qf[j][0], qf[j][1]);
+        mma<T>(s2, k1, qf[4 + j][0], qf[4 + j][1]);
       }
-      uint4 v[2][2][2];                              // [token half][token][dimension half]
+      // ---- scores in units of ln 2 after `c`: s[0], s[1] token g, s[2], s[3] token 8 + g; queries 2 t4, 2 t4 + 1
+      float c = unit_scale;
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int i = 0; i < 4; ++i) s[i] += s2[i];
+      if (!plain) {
+        if (a.cap > 0.0f) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < 4; ++i) s[i] = cap_out * tanh_of(s[i] * cap_in);
+        } else {
 #pragma unroll
-          for (int d = 0; d < 2; ++d) v[e][i][d] = lds_16(at + e * kHalf + v_off[i][d]);
-      const int t_unit = first_token(cur);
-      const uint32_t ok = good >> 2 * stage;
-      const bool edge = t_unit < cur.ext.lo || t_unit + kUnit > cur.ext.n || (ok & 3u) != 3u;
-      __syncwarp();                                  // every lane has read the stage
-      issue(stage);
-      // ---- scores in units of ln 2: s[0], s[1] row g, s[2], s[3] row 8 + g; queries 2 t4, 2 t4 + 1
-      if (a.cap > 0.0f) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = a.cap * kLog2e * tanhf(s[i] * a.scale / a.cap);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] *= a.scale * kLog2e;
-      }
-      const int tok = t_unit + token_of_row(g);
-      if (a.slopes) {
-        const float back0 = static_cast<float>(tok - (cur.ext.n - 1)), back1 = static_cast<float>(tok + 8 - (cur.ext.n - 1));
+          for (int i = 0; i < 4; ++i) s[i] *= c;
+        }
+        const float back0 = static_cast<float>(ua.x + g - (ua.z - 1)), back1 = static_cast<float>(ua.x + g + 8 - (ua.z - 1));
         s[0] = fmaf(slope0, back0, s[0]);
         s[1] = fmaf(slope1, back0, s[1]);
         s[2] = fmaf(slope0, back1, s[2]);
         s[3] = fmaf(slope1, back1, s[3]);
+        c = 1.0f;
       }
-      if (edge) {
-        if (!(ok & 1u) || tok < cur.ext.lo || tok >= cur.ext.n) s[0] = s[1] = -INFINITY;
-        if (!(ok & 2u) || tok + 8 < cur.ext.lo || tok + 8 >= cur.ext.n) s[2] = s[3] = -INFINITY;
+      if (edge || c < 0.0f) {
+        // (a scale below 0 would turn the masked scores around: apply it first)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {              // a masked token's weight is 0, but 0 x NaN is not
-            const int t = t_unit + 8 * e + token_of_row(2 * t4 + i);
-            if (!(ok >> e & 1u) || t < cur.ext.lo || t >= cur.ext.n) v[e][i][0] = v[e][i][1] = make_uint4(0, 0, 0, 0);
-          }
+        for (int i = 0; i < 4; ++i) s[i] *= c;
+        c = 1.0f;
+        if (!(ua.w & 1) || ua.x + g < ua.y || ua.x + g >= ua.z) s[0] = s[1] = -INFINITY;
+        if (!(ua.w & 2) || ua.x + g + 8 < ua.y || ua.x + g + 8 >= ua.z) s[2] = s[3] = -INFINITY;
       }
       // ---- the running reference of the exponents follows the maximum only when that is 2^8 past it
-      const float top0 = fmaxf(s[0], s[2]), top1 = fmaxf(s[1], s[3]);
+      const float top0 = fmaxf(s[0], s[2]) * c, top1 = fmaxf(s[1], s[3]) * c;
       if (__any_sync(0xffffffffu, top0 > m0 + 8.0f || top1 > m1 + 8.0f)) {
         float n0 = fmaxf(m0, top0), n1 = fmaxf(m1, top1);
 #pragma unroll
@@ -536,10 +566,10 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
       }
       const float base0 = m0 == -INFINITY ? 0.0f : m0 - Parts<T>::kShift;
       const float base1 = m1 == -INFINITY ? 0.0f : m1 - Parts<T>::kShift;
-      s[0] = exp2_of(s[0] - base0);
-      s[1] = exp2_of(s[1] - base1);
-      s[2] = exp2_of(s[2] - base0);
-      s[3] = exp2_of(s[3] - base1);
+      s[0] = exp2_of(fmaf(s[0], c, -base0));
+      s[1] = exp2_of(fmaf(s[1], c, -base1));
+      s[2] = exp2_of(fmaf(s[2], c, -base0));
+      s[3] = exp2_of(fmaf(s[3], c, -base1));
       l0 += s[0] + s[2];
       l1 += s[1] + s[3];
       uint32_t w[2][Parts<T>::kN];
@@ -550,28 +580,24 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
         w[0][i] = transposed(w[0][i]);
         w[1][i] = transposed(w[1][i]);
       }
-      // ---- rows 8 g + i and 64 + 8 g + i of V^T
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        uint32_t f[4];
+        uint32_t v[4];
+        ldsm_t(v, base + (i / 4) * h_off + (v_at ^ 32 * (i % 4)));
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            const uint32_t y0 = reinterpret_cast<const uint32_t*>(&v[e][0][d])[i / 2];
-            const uint32_t y1 = reinterpret_cast<const uint32_t*>(&v[e][1][d])[i / 2];
-            f[2 * e + d] = __byte_perm(y0, y1, i % 2 ? 0x7632 : 0x5410);
-          }
-#pragma unroll
-        for (int y = 0; y < Parts<T>::kN; ++y) mma<T>(acc[i], f[0], f[1], f[2], f[3], w[0][y], w[1][y]);
+        for (int y = 0; y < Parts<T>::kN; ++y) mma<T>(acc[i], v, w[0][y], w[1][y]);
+      }
+      __syncwarp();                                  // every lane has read the stage
+      if (lane == 0) ptx::mbar_arrive(&s_free[warp][stage]);
+      if (++stage == kStages) {
+        stage = 0;
+        phase ^= 1;
       }
 
-      const bool ends = cur.u == cur.ext.units - 1;
+      const bool ends = ub.z == ub.w - 1;
       if (ends || x + 1 == x_end) {                  // the segment's or the share's last unit
-        Walk next = cur;
-        step(next);
-        if (x + 1 < x_end) load_q(next);
-        const bool begins = x - cur.u >= x_begin;
+        fresh = true;
+        const bool begins = x - ub.z >= x_begin;
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
           l0 += __shfl_xor_sync(0xffffffffu, l0, o);
@@ -579,82 +605,66 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
         }
         l0 *= kUnshift;
         l1 *= kUnshift;
-        const int h = cur.seg / seg_blocks, head0 = h * a.group + (cur.seg % seg_blocks) * kSegHeads;
-        const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int q = 2 * t4 + c;
-          const int64_t out_row = static_cast<int64_t>(cur.b) * a.n_q + head0 + q;
-          const float m = c ? m1 : m0, l = c ? l1 : l0;
-          float f = kUnshift, fp = 0.0f, base = 0.0f, total = l;
+        for (int i = 0; i < 2; ++i) {
+          const int q = 2 * t4 + i;
+          const int64_t out_row = static_cast<int64_t>(ub.x) * a.n_q + head0 + q;
+          const float m = i ? m1 : m0, l = i ? l1 : l0;
           if (begins && ends) {
             const float prior = a.prior_lse && q < n_g ? a.prior_lse[out_row] * kLog2e : -INFINITY;
-            base = fmaxf(m, prior);
-            if (base == -INFINITY) base = 0.0f;
-            const float fm = exp2_of(m - base);
-            fp = exp2_of(prior - base);
-            total = fmaf(l, fm, fp);
-            f *= fm;
-          }
-          const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-          __syncwarp();                              // (the log-sum may be written over the prior's)
+            float top = fmaxf(m, prior);
+            if (top == -INFINITY) top = 0.0f;
+            const float fm = exp2_of(m - top), fp = exp2_of(prior - top);
+            const float total = fmaf(l, fm, fp), inv = total == 0.0f ? 0.0f : 1.0f / total;
+            __syncwarp();                            // (the log-sum may be written over the prior's)
+            if (q < n_g) {
+              float* to = a.out + out_row * D + g;
+              float o[16];
 #pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            float o[8];
+              for (int j = 0; j < 16; ++j) o[j] = acc[j / 2][2 * (j % 2) + i] * (fm * kUnshift);
+              if (fp > 0.0f) {                       // (all loads before the stores, which may go to the same place)
+                float from[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = acc[i][2 * d + c] * f;
-            if (begins && ends) {
-              if (q >= n_g) continue;
-              float* to = a.out + out_row * D + 64 * d + 8 * g;
-              const float* from = a.prior_out + out_row * D + 64 * d + 8 * g;
+                for (int j = 0; j < 16; ++j) from[j] = a.prior_out[out_row * D + g + 8 * j];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] = (fp > 0.0f ? fmaf(fp, from[i], o[i]) : o[i]) * inv;
-              *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
-              *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
-            } else {
-              float* to = &piece_at(warp, begins)->sum[q][64 * d + 8 * g];
-              *reinterpret_cast<float4*>(to) = make_float4(o[0], o[1], o[2], o[3]);
-              *reinterpret_cast<float4*>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+                for (int j = 0; j < 16; ++j) o[j] = fmaf(fp, from[j], o[j]);
+              }
+#pragma unroll
+              for (int j = 0; j < 16; ++j) to[8 * j] = o[j] * inv;
+              if (a.lse && g == 0) a.lse[out_row] = top * kLn2 + logf(total);
             }
-          }
-          if (g == 0) {
-            if (begins && ends) {
-              if (a.lse && q < n_g) a.lse[out_row] = base * kLn2 + logf(total);
-            } else {
-              piece_at(warp, begins)->top[q] = m;
-              piece_at(warp, begins)->total[q] = l;
+          } else {
+            Piece* to = piece_at(warp, begins);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) to->sum[q][8 * j + g] = acc[j / 2][2 * (j % 2) + i] * kUnshift;
+            if (g == 0) {
+              to->top[q] = m;
+              to->total[q] = l;
             }
           }
         }
-        if (!(begins && ends) && lane == 0)
-          s_of[warp][begins] = {cur.b, cur.seg, ends, x - cur.u + cur.ext.units - 1};
+        if (!(begins && ends) && lane == 0) s_of[warp][begins] = {ub.x, ub.y, ends, x - ub.z + ub.w - 1};
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
         m0 = m1 = -INFINITY;
         l0 = l1 = 0.0f;
       }
-      if (x + 1 < x_end) step(cur);
-      if (++stage == kStages) {
-        stage = 0;
-        phase ^= 1;
-      }
-    }
-    if (dead) {                                      // a copy did not arrive: tell, and wait out those under way
-      if (lane == 0) raise(p.err, kTimeout);
-      for (++x; x < x_ahead; ++x) {
-        if (++stage == kStages) {
-          stage = 0;
-          phase ^= 1;
-        }
-        ptx::mbar_wait_bounded(&s_full[warp][stage], phase, &s_abort);
-      }
     }
   }
   __syncthreads();
+  if (s_abort) {                                     // copies under way write to this CTA's memory: wait them out
+    if (tid == 0) {
+      const uint64_t t0 = ptx::globaltimer_ns();
+      while (ptx::globaltimer_ns() - t0 < 100000000ull) __nanosleep(1000000);
+    }
+    __syncthreads();
+    return;
+  }
 
   // ---- join the warps' pieces, which are in the order of the units
+  if (warp >= kW) return;
   const PieceOf* of = s_of[0];
-  const int dim = tid % D;                           // a thread takes this dimension of every (kT / D)-th head
+  const int dim = tid % D;                           // a thread takes this dimension of every second head
   for (int i = 0; i < 2 * kW; ++i) {
     const PieceOf one = of[i];
     if (one.b < 0) continue;
@@ -665,7 +675,7 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, kDecodeCtas)
     const int h = one.seg / seg_blocks, head0 = h * a.group + (one.seg % seg_blocks) * kSegHeads;
     const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
     float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + begins) * kPiece;
-    for (int q = tid / D; q < n_g; q += kT / D) {
+    for (int q = tid / D; q < n_g; q += kW * 32 / D) {
       const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
       const float prior = whole && a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
       float top = prior;
@@ -806,22 +816,20 @@ cudaError_t launch_append(int dtype, const AppendArgs& a, cudaStream_t st) {
 }
 
 size_t decode_workspace(int num_sms) {
-  const size_t ctas = static_cast<size_t>(std::max(1, num_sms)) * kDecodeCtas;
-  return ctas * (2 * kPiece * sizeof(float) + sizeof(int4));
+  return static_cast<size_t>(std::max(1, num_sms)) * (2 * kPiece * sizeof(float) + sizeof(int4));
 }
 
 cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
-  const int ctas = std::max(1, a.num_sms) * kDecodeCtas;
+  const int ctas = std::max(1, a.num_sms);
   const auto kernel = dtype == AATC_BF16 ? aatc_paged_decode_kernel<__nv_bfloat16> : aatc_paged_decode_kernel<__half>;
-  // pages as rows of 128 bytes, two a token; a box is a unit's tokens in a page
-  CUtensorMap map;
-  const uint64_t rows = static_cast<uint64_t>(4) * a.pool.n_kv << a.pool.page_shift;
-  cudaError_t e = make_tensor_map_3d(&map, a.pool.pages, D / 2, rows, a.pool.n_pages, D, rows * D, D / 2,
-                                     2 * std::min(kUnit, 1 << a.pool.page_shift));
+  CUtensorMap map;                  // [page][token of a head of keys or values][128]
+  const uint64_t tokens = static_cast<uint64_t>(2) * a.pool.n_kv << a.pool.page_shift;
+  cudaError_t e = make_tensor_map_3d(&map, a.pool.pages, D, tokens, a.pool.n_pages, 2 * kRow, 2 * kRow * tokens, D / 2,
+                                     std::min(kUnit, 1 << a.pool.page_shift));
   if (e != cudaSuccess) return e;
   e = ensure_smem_optin(reinterpret_cast<const void*>(kernel), kDecodeSmem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kernel, dim3(ctas), dim3(kDecodeWarps * 32), kDecodeSmem, st, a, map);
+  e = launch_pdl(kernel, dim3(ctas), dim3(kDecodeThreads), kDecodeSmem, st, a, map);
   if (e != cudaSuccess) return e;
   return launch_pdl(aatc_paged_join_kernel, dim3(ctas, std::min(a.group, kSegHeads)), dim3(kJoinWarps * 32), 0, st, a, ctas);
 }
