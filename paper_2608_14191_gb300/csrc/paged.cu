@@ -120,9 +120,9 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
 
 // ---------------------------------------------------------------- decode attention
 // The work of a call is its units of 16 tokens: those of sequence 0's kv-head 0, then kv-head 1, ...,
-// then sequence 1's, a (sequence, kv-head) being a segment.  CTA c of n takes the units
-// [c U / n, (c + 1) U / n) of all U and each of its consumer warps an eighth of those, so every warp has the
-// same share whatever the lengths.  A segment that lies inside a warp's share is finished by the warp, the
+// then sequence 1's, a (sequence, kv-head) being a segment.  They are laid out on a line, with a gap before
+// every segment for what its begin and end cost a warp; every CTA takes an equal part of the line
+// and each of its consumer warps an eighth of that, so the shares are alike whatever the lengths.  A segment that lies inside a warp's share is finished by the warp, the
 // pieces of one that lies in several warps are joined in shared memory, and those of one in several CTAs
 // through the workspace by the second launch.  (Query heads beyond eight of a kv-head are further segments over
 // the same tokens.)  One more warp brings the units: a lane of it walks each consumer's share, across
@@ -132,11 +132,12 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
 constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM
-constexpr int kProducers = 4;       // producer warps
+constexpr int kProducers = 2;       // producer warps
 constexpr int kServes = kConsumers / kProducers;
 constexpr int kDecodeThreads = (kConsumers + kProducers) * 32;
 constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less
-constexpr int kStages = 3;          // units of a consumer on their way: keys and values, 8 KB each
+constexpr int kStages = 2;          // units of a consumer on their way: keys and values, 8 KB each
+constexpr int kGap = 3;             // units' time that a segment costs beside its units
 constexpr int kRow = 128;           // bytes of half a token's key or value: a row in shared memory
 constexpr int kStage = kUnit * 4 * kRow;      // keys, then values
 constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128], maxima [8], totals [8]
@@ -144,9 +145,18 @@ constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128
 // Workspace: pieces [2 n_ctas] (CTA c's share begins inside a segment: piece 2 c; ends inside one that it began:
 // 2 c + 1), then int4 per CTA: the segment that it began and did not end (sequence, segment of the
 // sequence, last CTA with a piece of it; sequence -1: none).
+// The line in even parts: CTA c has [begin(c), begin(c + 1)).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {   // (both >= 0; a 64-bit division is 100 instructions)
+  return (a | b) >> 32 ? a / b : static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+}
 struct Share {
-  int64_t total;                    // units
-  int n_ctas;                       // CTAs that get any
+  int64_t each;
+  int n_ctas, longer;               // CTAs that get anything; the first of them get one more
+  __device__ int64_t begin(int c) const { return c * each + min(c, longer); }
+  __device__ int cta_of(int64_t at) const {
+    const int64_t big = longer * (each + 1);
+    return static_cast<int>(at < big ? quotient(at, each + 1) : longer + quotient(at - big, each));
+  }
 };
 
 template <typename T>
@@ -243,11 +253,6 @@ __device__ __forceinline__ Extent extent_of(const DecodeArgs& a, int len) {
   return e;
 }
 
-// Unit u of all is in the share of CTA ((u + 1) n - 1) / U.
-__device__ __forceinline__ int cta_of(const Share& s, int64_t unit) {
-  return static_cast<int>(((unit + 1) * s.n_ctas - 1) / s.total);
-}
-
 // What a consumer learns of a unit: its first token, the live ones [lo, n) of its sequence, whether the pages of
 // its halves are in the pool (bits 0, 1 of `ok`), and where it belongs.
 struct __align__(16) Unit {
@@ -263,7 +268,7 @@ struct Piece {
 struct PieceOf {
   int b, seg;                       // b < 0: none
   int ends;
-  int64_t last_unit;                // of the segment, among all units
+  int64_t last_unit;                // of the segment, on the line
 };
 
 // Shared memory: every consumer's ring of stages, which its piece of the segment that it began takes over at the
@@ -311,11 +316,11 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 
   // ---- the total, and the sequences in which the warps' shares begin: prefix sums over kT sequences at a time
   int len = 0;
-  int64_t units = 0, upto = 0;                       // of sequence i0 + tid; up to it within the chunk
+  int64_t units = 0, upto = 0;                       // of sequence i0 + tid, with its gaps; up to it within the chunk
   auto scan = [&](int i0) {
     const int i = i0 + tid;
     len = i < a.batch ? __ldg(a.lens + i) : 0;
-    units = i < a.batch ? static_cast<int64_t>(extent_of(a, len).units) * n_seg : 0;
+    units = i < a.batch ? static_cast<int64_t>(extent_of(a, len).units + kGap) * n_seg : 0;
     upto = units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -333,22 +338,23 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     }
     return sum;
   };
-  Share share;
-  share.total = 0;
+  int64_t total = 0;
   for (int i0 = 0; i0 < a.batch; i0 += kT) {
-    share.total += scan(i0);
+    total += scan(i0);
     if (blockIdx.x == 0 && i0 + tid < a.batch && (len < 0 || len > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
   }
-  share.n_ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (share.total + kUnitsPerCta - 1) / kUnitsPerCta));
+  Share share;
+  share.n_ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kUnitsPerCta - 1) / kUnitsPerCta));
   if (tid == 0) desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
   if (blockIdx.x >= share.n_ctas) return;
-  const int64_t first = blockIdx.x * share.total / share.n_ctas;
-  const int64_t here = (blockIdx.x + 1) * share.total / share.n_ctas - first;
+  share.each = quotient(total, share.n_ctas);
+  share.longer = static_cast<int>(total - share.each * share.n_ctas);
+  const int64_t first = share.begin(blockIdx.x), here = share.begin(blockIdx.x + 1) - first;
   {
     const int64_t begin_last = first + here * (kW - 1) / kW;
     int64_t before = 0;
     for (int i0 = 0; i0 < a.batch; i0 += kT) {
-      const int64_t sum = a.batch > kT ? scan(i0) : share.total;
+      const int64_t sum = a.batch > kT ? scan(i0) : total;
 #pragma unroll
       for (int w = 0; w < kW; ++w) {
         const int64_t y = first + here * w / kW - before;
@@ -364,6 +370,17 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     __syncthreads();
   }
 
+  // Where on the line a consumer's share begins: the segment of sequence s_seq and the first unit there, whose place is
+  // moved past the gap.
+  auto begin_of = [&](int w, int64_t& x, Walk& at) {
+    at.b = s_seq[w];
+    at.ext = extent_of(a, s_len[w]);
+    const int64_t in_seq = x - s_before[w];
+    at.seg = static_cast<int>(quotient(in_seq, at.ext.units + kGap));
+    const int in_seg = static_cast<int>(in_seq - static_cast<int64_t>(at.seg) * (at.ext.units + kGap));
+    at.u = max(0, in_seg - kGap);
+    x += max(0, kGap - in_seg);
+  };
   // second eight tokens and second halves of the heads in a stage
   const int e_off = p.page_shift > 3 ? 8 * kRow : 16 * kRow, h_off = p.page_shift > 3 ? 16 * kRow : 8 * kRow;
   if (warp >= kW) {
@@ -371,12 +388,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     const bool serves = lane < kServes;
     const int w = (warp - kW) * kServes + (serves ? lane : 0);
     int64_t x = first + here * w / kW;
-    const int64_t x_end = serves ? first + here * (w + 1) / kW : x;
+    const int64_t x_end = serves ? first + here * (w + 1) / kW : 0;
     Walk at;
-    at.b = s_seq[w];
-    at.ext = extent_of(a, s_len[w]);
-    at.seg = static_cast<int>((x - s_before[w]) / at.ext.units);
-    at.u = static_cast<int>((x - s_before[w]) % at.ext.units);
+    begin_of(w, x, at);
     at.len_next = at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
     int id0 = -1, id1 = -1;                          // pages of the unit's halves
     auto fetch_ids = [&]() {
@@ -423,12 +437,14 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
           if (ok0) copy(to, id0);
           if (ok1) copy(to + e_off, id1);
         }
-        if (++x < x_end && ++at.u == at.ext.units) {
+        ++x;
+        if (++at.u == at.ext.units) {
           at.u = 0;
+          x += kGap;
           if (++at.seg == n_seg) {
             at.seg = 0;
             ++at.b;
-            at.ext = extent_of(a, at.len_next);
+            at.ext = extent_of(a, at.len_next);      // (of nothing past the last sequence)
             at.len_next = at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
           }
         }
@@ -450,7 +466,10 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     // ---- a consumer
     const int g = lane / 4, t4 = lane % 4;
     int64_t x = first + here * warp / kW;
-    const int64_t x_begin = x, x_end = first + here * (warp + 1) / kW;
+    const int64_t x_end = first + here * (warp + 1) / kW;
+    Walk at;
+    begin_of(warp, x, at);
+    const int64_t x_begin = x;
     unsigned char* ring = rings + warp * (kStages * kStage);
     // Rows of 128 bytes: [half of the head's values][token] of a page's eight or sixteen tokens, their 16-byte pieces permuted
     // by the row's number modulo 8.  Keys: matrices (tokens 0 .. 7, 8 .. 15) x (piece, next piece), the A operand of
@@ -460,7 +479,18 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     const uint32_t v_at = kStage / 2 + (lane / 16) * e_off + lane % 8 * kRow + ((lane / 8 % 2) ^ lane % 8) * 16;
     const float unit_scale = a.scale * kLog2e, cap_in = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap_out = a.cap * kLog2e;
     const bool plain = a.cap <= 0.0f && !a.slopes;
-    uint32_t qf[8][2];                               // B operand of the score MMAs: column g
+    uint32_t qf[8][2], q_next[8][2];                 // B operand of the score MMAs: column g; of the next segment
+    auto load_q = [&](int b, int seg, uint32_t (&to)[8][2]) {
+      const int h = seg / seg_blocks, head0 = h * a.group + (seg % seg_blocks) * kSegHeads;
+      const T* q = static_cast<const T*>(a.q.x) + b * a.q.token_stride + (head0 + g) * a.q.head_stride + 2 * t4;
+      const bool in = g < min(kSegHeads, (h + 1) * a.group - head0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        to[j][0] = in ? *reinterpret_cast<const uint32_t*>(q + 16 * j) : 0u;
+        to[j][1] = in ? *reinterpret_cast<const uint32_t*>(q + 16 * j + 8) : 0u;
+      }
+    };
+    if (x < x_end) load_q(at.b, at.seg, q_next);
     float slope0 = 0.0f, slope1 = 0.0f;
     float acc[8][4];                                 // dimensions 16 i + g, 16 i + 8 + g; queries 2 t4, 2 t4 + 1
 #pragma unroll
@@ -469,7 +499,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     int stage = 0;
     uint32_t phase = 0;
     bool fresh = true;                               // the next unit is of another segment
-    for (; x < x_end; ++x) {
+    while (x < x_end) {
       if (!ptx::mbar_wait_bounded(&s_full[warp][stage], phase, &s_abort)) {
         if (lane == 0) {                             // a copy did not arrive: tell, and stop the others
           raise(p.err, kTimeout);
@@ -481,12 +511,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       const int4 ub = *reinterpret_cast<const int4*>(&s_unit[warp][stage].b);      // b, seg, u, units
       const int h = ub.y / seg_blocks, head0 = h * a.group + (ub.y % seg_blocks) * kSegHeads;
       const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
+      const bool ends = ub.z == ub.w - 1;
+      const int64_t x_next = x + (ends ? 1 + kGap : 1);
       if (fresh) {
-        const T* q = static_cast<const T*>(a.q.x) + ub.x * a.q.token_stride + (head0 + g) * a.q.head_stride + 2 * t4;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          qf[j][0] = g < n_g ? *reinterpret_cast<const uint32_t*>(q + 16 * j) : 0u;
-          qf[j][1] = g < n_g ? *reinterpret_cast<const uint32_t*>(q + 16 * j + 8) : 0u;
+          qf[j][0] = q_next[j][0];
+          qf[j][1] = q_next[j][1];
         }
         if (a.slopes) {
           slope0 = 2 * t4 < n_g ? a.slopes[head0 + 2 * t4] * kLog2e : 0.0f;
@@ -494,6 +525,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         }
         fresh = false;
       }
+      if (ends && x_next < x_end) load_q(ub.y + 1 < n_seg ? ub.x : ub.x + 1, ub.y + 1 < n_seg ? ub.y + 1 : 0, q_next);
       const uint32_t base = ptx::smem_u32(ring) + stage * kStage;
       const bool edge = ua.x < ua.y || ua.x + kUnit > ua.z || ua.w != 3;
       if (edge) {                                    // values of masked tokens: their weight is 0, but 0 x NaN is not
@@ -594,8 +626,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         phase ^= 1;
       }
 
-      const bool ends = ub.z == ub.w - 1;
-      if (ends || x + 1 == x_end) {                  // the segment's or the share's last unit
+      if (ends || x_next >= x_end) {                 // the segment's or the share's last unit
         fresh = true;
         const bool begins = x - ub.z >= x_begin;
 #pragma unroll
@@ -649,6 +680,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         m0 = m1 = -INFINITY;
         l0 = l1 = 0.0f;
       }
+      x = x_next;
     }
   }
   __syncthreads();
@@ -668,9 +700,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   for (int i = 0; i < 2 * kW; ++i) {
     const PieceOf one = of[i];
     if (one.b < 0) continue;
-    int n = i;                                       // the last piece of the same segment
-    for (int j = i + 1; j < 2 * kW; ++j)
-      if (of[j].b == one.b && of[j].seg == one.seg) n = j;
+    const uint32_t same = __ballot_sync(0xffffffffu, lane < 2 * kW && of[lane % (2 * kW)].b == one.b &&
+                                                         of[lane % (2 * kW)].seg == one.seg);
+    const int n = 31 - __clz(same);                  // the last piece of the segment
     const bool begins = i % 2, whole = begins && of[n].ends;
     const int h = one.seg / seg_blocks, head0 = h * a.group + (one.seg % seg_blocks) * kSegHeads;
     const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
@@ -678,68 +710,93 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     for (int q = tid / D; q < n_g; q += kW * 32 / D) {
       const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
       const float prior = whole && a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
-      float top = prior;
-      for (int j = i; j <= n; ++j)
-        if (of[j].b >= 0) top = fmaxf(top, piece_at(j / 2, j % 2)->top[q]);
+      const float prior_out = prior > -INFINITY ? a.prior_out[out_row * D + dim] : 0.0f;
+      float tops[2 * kW], top = prior;
+#pragma unroll
+      for (int j = 0; j < 2 * kW; ++j) {
+        tops[j] = same >> j & 1 ? piece_at(j / 2, j % 2)->top[q] : -INFINITY;
+        top = fmaxf(top, tops[j]);
+      }
       const float base = top == -INFINITY ? 0.0f : top;
-      float sum = 0.0f, total = 0.0f;
-      for (int j = i; j <= n; ++j)
-        if (of[j].b >= 0) {
-          const Piece* one_of = piece_at(j / 2, j % 2);
-          const float f = exp2_of(one_of->top[q] - base);
-          sum = fmaf(f, one_of->sum[q][dim], sum);
-          total = fmaf(f, one_of->total[q], total);
+      float sum = 0.0f, all = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 2 * kW; ++j)
+        if (same >> j & 1) {
+          const float f = exp2_of(tops[j] - base);
+          sum = fmaf(f, piece_at(j / 2, j % 2)->sum[q][dim], sum);
+          all = fmaf(f, piece_at(j / 2, j % 2)->total[q], all);
         }
       if (whole) {
         if (prior > -INFINITY) {
           const float f = exp2_of(prior - base);
-          sum = fmaf(f, a.prior_out[out_row * D + dim], sum);
-          total += f;
+          sum = fmaf(f, prior_out, sum);
+          all += f;
         }
-        a.out[out_row * D + dim] = total == 0.0f ? 0.0f : sum / total;
+        a.out[out_row * D + dim] = all == 0.0f ? 0.0f : sum / all;
         asm volatile("bar.sync %0, %1;" ::"r"(1 + tid / D), "n"(D) : "memory");   // (the log-sum may replace the prior's)
-        if (a.lse && dim == 0) a.lse[out_row] = base * kLn2 + logf(total);
+        if (a.lse && dim == 0) a.lse[out_row] = base * kLn2 + logf(all);
       } else {
         piece[q * D + dim] = sum;
         if (dim == 0) {
           piece[kSegHeads * D + q] = top;
-          piece[kSegHeads * D + kSegHeads + q] = total;
+          piece[kSegHeads * D + kSegHeads + q] = all;
         }
       }
     }
-    if (begins && !whole && tid == 0) desc[blockIdx.x] = make_int4(one.b, one.seg, cta_of(share, one.last_unit), 0);
+    if (begins && !whole && tid == 0) desc[blockIdx.x] = make_int4(one.b, one.seg, share.cta_of(one.last_unit), 0);
     i = n;
   }
 }
 
-// Joins the pieces of the segments that CTA blockIdx.x of the first launch began and did not end; one CTA
-// a query head, a warp takes every eighth piece, a lane four dimensions.
+// Joins the pieces of the segment that CTA blockIdx.x of the first launch began and did not end; one CTA
+// a query head.  A warp takes every eighth piece, a lane four dimensions, four pieces' loads at a time.
 constexpr int kJoinWarps = 8;
 __global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const DecodeArgs a, int n_ctas) {
   __shared__ float so[kJoinWarps][D];
   __shared__ float sm[kJoinWarps], sl[kJoinWarps];
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, q = blockIdx.y, c0 = blockIdx.x;
+  const int seg_blocks = (a.group + kSegHeads - 1) / kSegHeads;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int4 what = __ldcg(reinterpret_cast<const int4*>(a.ws + static_cast<size_t>(n_ctas) * 2 * kPiece) + blockIdx.x);
-  if (what.x < 0) return;
-  const int seg_blocks = (a.group + kSegHeads - 1) / kSegHeads, h = what.y / seg_blocks;
-  const int head = h * a.group + (what.y % seg_blocks) * kSegHeads + blockIdx.y;
-  if (head >= (h + 1) * a.group) return;
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, q = blockIdx.y;
-  const int c0 = blockIdx.x, n = what.z - c0 + 1;                // pieces 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
+  const int4 what = __ldcg(reinterpret_cast<const int4*>(a.ws + static_cast<size_t>(n_ctas) * 2 * kPiece) + c0);
+  const int h = what.y / seg_blocks, head = h * a.group + (what.y % seg_blocks) * kSegHeads + q;
+  if (what.x < 0 || head >= (h + 1) * a.group) return;
+  const int n = what.z - c0 + 1;                                  // pieces 2 c0 + 1, 2 (c0 + 1), 2 (c0 + 2), ...
+  const int64_t out_row = static_cast<int64_t>(what.x) * a.n_q + head;
+  const float prior = a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
+  const float prior_out = a.prior_lse && tid < D ? a.prior_out[out_row * D + tid] : 0.0f;
   float top = -INFINITY, total = 0.0f;
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int i = warp; i < n; i += kJoinWarps) {
-    const float* piece = a.ws + (static_cast<size_t>(c0 + i) * 2 + (i == 0 ? 1 : 0)) * kPiece;
-    const float m = __ldcg(piece + kSegHeads * D + q), l = __ldcg(piece + kSegHeads * D + kSegHeads + q);
-    const float4 o = __ldcg(reinterpret_cast<const float4*>(piece + q * D) + lane);
-    const float next = fmaxf(top, m), base = next == -INFINITY ? 0.0f : next;
-    const float r = exp2_of(top - base), f = exp2_of(m - base);
-    total = fmaf(total, r, f * l);
-    sum.x = fmaf(sum.x, r, f * o.x);
-    sum.y = fmaf(sum.y, r, f * o.y);
-    sum.z = fmaf(sum.z, r, f * o.z);
-    sum.w = fmaf(sum.w, r, f * o.w);
+  constexpr int kAtOnce = 4;
+  for (int i0 = warp; i0 < n; i0 += kJoinWarps * kAtOnce) {
+    float m[kAtOnce], l[kAtOnce];
+    float4 o[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = i0 + k * kJoinWarps;
+      const float* piece = a.ws + (static_cast<size_t>(c0 + i) * 2 + (i == 0 ? 1 : 0)) * kPiece;
+      m[k] = i < n ? __ldcg(piece + kSegHeads * D + q) : -INFINITY;
+      l[k] = i < n ? __ldcg(piece + kSegHeads * D + kSegHeads + q) : 0.0f;
+      o[k] = i < n ? __ldcg(reinterpret_cast<const float4*>(piece + q * D) + lane) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    float next = top;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, m[k]);
+    const float base = next == -INFINITY ? 0.0f : next, r = exp2_of(top - base);
+    total *= r;
+    sum.x *= r;
+    sum.y *= r;
+    sum.z *= r;
+    sum.w *= r;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const float f = exp2_of(m[k] - base);
+      total = fmaf(f, l[k], total);
+      sum.x = fmaf(f, o[k].x, sum.x);
+      sum.y = fmaf(f, o[k].y, sum.y);
+      sum.z = fmaf(f, o[k].z, sum.z);
+      sum.w = fmaf(f, o[k].w, sum.w);
+    }
     top = next;
   }
   *reinterpret_cast<float4*>(&so[warp][4 * lane]) = sum;
@@ -747,8 +804,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const 
     sm[warp] = top;
     sl[warp] = total;
   }
-  const int64_t out_row = static_cast<int64_t>(what.x) * a.n_q + head;
-  const float prior = a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
   __syncthreads();
   if (tid >= D) return;
   top = prior;
@@ -764,7 +819,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const 
   }
   if (prior > -INFINITY) {
     const float f = exp2_of(prior - base);
-    s = fmaf(f, a.prior_out[out_row * D + tid], s);
+    s = fmaf(f, prior_out, s);
     l += f;
   }
   a.out[out_row * D + tid] = l == 0.0f ? 0.0f : s / l;
