@@ -1,6 +1,7 @@
 """Build the in-tree CUDA library ``libaatc.so`` for sm_103a with nvcc (no cmake).
 
-Each translation unit compiles in parallel; the shared object lands next to this file.
+Each translation unit compiles in parallel; the shared object lands next to this file, and with it
+``_calls.so``, the Python extension through which the binding makes the paged calls.
 """
 from __future__ import annotations
 
@@ -9,14 +10,17 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libaatc.so")
+CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["planner.cpp", "planfile.cpp", "capi.cpp", "encode.cu", "decode.cu", "prefill.cu", "group.cu", "paged_api.cpp", "paged.cu",
            "selftest.cu"]
+CALLS_SOURCE = "pycalls.cpp"
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -35,6 +39,8 @@ def _flags():
 def _compile(src: str, verbose: bool) -> str:
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
     cmd = [_nvcc()] + _flags() + ["-c", os.path.join(CSRC, src), "-o", obj]
+    if src == CALLS_SOURCE:
+        cmd += ["-I" + sysconfig.get_paths()["include"]]
     if src.endswith(".cu") and verbose:
         cmd += ["-Xptxas", "-v"]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -48,19 +54,24 @@ def _compile(src: str, verbose: bool) -> str:
 def build(verbose: bool = False, force: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "aatc.h")]
-    if not force and os.path.exists(LIB):
+    if not force and os.path.exists(LIB) and os.path.exists(CALLS):
         newest = max(os.path.getmtime(p) for p in deps)
-        if os.path.getmtime(LIB) >= newest:
+        if os.path.getmtime(LIB) >= newest and os.path.getmtime(CALLS) >= newest:
             return LIB
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
-        objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
-    tmp = LIB + ".tmp"
-    cmd = [_nvcc()] + ARCH + ["-shared", "-o", tmp] + objs + ["-lpthread", "-ldl", "-lrt"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    sources = SOURCES + [CALLS_SOURCE]
+    with cf.ThreadPoolExecutor(max_workers=len(sources)) as ex:
+        objs = list(ex.map(lambda s: _compile(s, verbose), sources))
+    _link(LIB, objs[:-1] + ["-lpthread", "-ldl", "-lrt"])
+    _link(CALLS, objs[-1:] + ["-L" + HERE, "-l:" + os.path.basename(LIB), "-Xlinker", "-rpath,$ORIGIN"])
+    return LIB
+
+
+def _link(out: str, args):
+    tmp = out + ".tmp"
+    r = subprocess.run([_nvcc()] + ARCH + ["-shared", "-o", tmp] + args, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, LIB)
-    return LIB
+    os.replace(tmp, out)
 
 
 if __name__ == "__main__":

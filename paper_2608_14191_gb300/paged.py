@@ -18,6 +18,10 @@ import torch
 
 from . import HEAD_DIM, _arg_error, _check, _dev_tensor, _on_device, _stream, load
 
+load()                  # (the extension is linked to the library)
+from . import _calls  # noqa: E402
+
+_calls.setup(torch.int32, torch.float32, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 _I32T, _F32T = torch.int32, torch.float32
 _SCALINGS = {"plain": (0, ()), "linear": (1, ()), "ntk": (2, ()), "ramp": (3, ("fast", "slow")),
@@ -76,7 +80,7 @@ class Rotary:
         self.rot_dim, self.layout, self.frequencies, self.factor = int(rot_dim), layout, freq, factor.value
         self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
         self._arg = _Rotary(self.turns.data_ptr(), self.rot_dim, int(layout == "interleaved"), self.factor)
-        self._ref = ctypes.byref(self._arg)
+        self._addr = ctypes.addressof(self._arg)
 
 
 class Pages:
@@ -99,10 +103,10 @@ class Pages:
         self.data, self.dtype, self.device = data, data.dtype, data.device
         self.n_layers, self.n_pages, _, self.n_kv_heads, self.page_size, _ = data.shape
         self._desc = _Desc(_TYPES[data.dtype], self.n_kv_heads, self.page_size, self.n_pages)
-        self._ref = ctypes.byref(self._desc)
+        self._addr = ctypes.addressof(self._desc)
         n = ctypes.c_size_t()
         self._lib = load()
-        _check(self._lib.aatc_pages_bytes(self._ref, ctypes.byref(n)), "aatc_pages_bytes")
+        _check(self._lib.aatc_pages_bytes(self._addr, ctypes.byref(n)), "aatc_pages_bytes")
         self.layer_bytes = n.value
         self._layers = [data.data_ptr() + i * n.value for i in range(self.n_layers)]
         self.flags = torch.zeros(1, dtype=_I32T, device=data.device)
@@ -118,7 +122,7 @@ class Pages:
         n = self._needs.get(n_q_heads)
         if n is None:
             got = ctypes.c_size_t()
-            _check(self._lib.aatc_paged_decode_workspace_bytes(self._ref, int(n_q_heads), ctypes.byref(got)),
+            _check(self._lib.aatc_paged_decode_workspace_bytes(self._addr, int(n_q_heads), ctypes.byref(got)),
                    "aatc_paged_decode_workspace_bytes")
             n = self._needs[n_q_heads] = got.value
         return n
@@ -136,65 +140,69 @@ class Pages:
         return f
 
 
-# Every call first checks all its arguments in one expression of cheap attribute reads, and only where that fails
-# goes through them one by one for the message (a call of a step costs the host as much as the GPU).
+# Every call first goes the short way, through the extension, which checks the common kinds of arguments and makes the
+# call; where it takes one of them for something else (None), the long way checks them one by one, with a
+# message for what is wrong, and makes the call through ctypes.
 
 def _heads(t, where: str, name: str, dtype, n_heads=None, n_tokens=None):
-    """Checks a [tokens][heads][128] argument."""
+    """Checks a [tokens][heads][128] argument; its pointer and strides."""
     _dev_tensor(t, where, name, dtype, 3, (n_tokens, n_heads, HEAD_DIM))
-    if t.stride()[2] != 1:
+    s = t.stride()
+    if s[2] != 1:
         _arg_error(where, f"the 128 values of a head of {name} must be contiguous")
+    return _Heads(t.data_ptr(), s[0], s[1])
 
 
-def _ints(t, where: str, name: str, n: int):
+def _ints(t, where: str, name: str, n: int) -> int:
     """Checks a contiguous int32 vector of n entries."""
     if not _on_device(t) or t.dtype != _I32T or t.shape != (n,) or not t.is_contiguous():
         _arg_error(where, f"{name} must be a contiguous device int32 tensor of {n} entries")
+    return t.data_ptr()
 
 
-def _floats(t, where: str, name: str, shape):
+def _floats(t, where: str, name: str, shape) -> int:
     if not _on_device(t) or t.dtype != _F32T or t.shape != shape or not t.is_contiguous():
         _arg_error(where, f"{name} must be a contiguous device float32 tensor of shape {tuple(shape)}")
+    return t.data_ptr()
 
 
 def _table(t, where: str, n_rows=None):
-    """Checks a block table [rows][max_pages]."""
+    """Checks a block table [rows][max_pages]; (pointer, rows, row stride, max_pages)."""
     if not _on_device(t) or t.dtype != _I32T or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         _arg_error(where, "table must be a device int32 tensor [rows][max_pages], rows contiguous")
-    if n_rows is not None and t.shape[0] != n_rows:
-        _arg_error(where, f"table must have {n_rows} rows, not {t.shape[0]}")
+    n, m = t.shape
+    if n_rows is not None and n != n_rows:
+        _arg_error(where, f"table must have {n_rows} rows, not {n}")
+    return t.data_ptr(), n, t.stride(0) if n > 1 else m, m
+
+
+def _pages(pages, where: str):
+    if not isinstance(pages, Pages):
+        _arg_error(where, "pages must be a Pages")
 
 
 def rotate(rope: Rotary, x, positions, out=None, backward: bool = False, stream=None):
     """aatc_rotate: x [tokens][heads][128] (bf16 or f16, strided) turned by positions (int32 [tokens]).
     out: None for a new tensor, or x itself.  backward: the gradient with respect to x, given out's."""
-    try:
-        n, h, d = x.shape
-        dtype = x.dtype
-        if out is None:
-            out = torch.empty((n, h, d), dtype=dtype, device=x.device)
-        xs, os = x.stride(), out.stride()
-        fine = (d == HEAD_DIM and x.is_cuda and dtype in _TYPES and xs[2] == 1 and out.is_cuda and out.dtype is dtype and
-                out.shape == x.shape and os[2] == 1 and positions.is_cuda and positions.dtype is _I32T and
-                positions.shape == (n,) and positions.is_contiguous() and isinstance(rope, Rotary))
-    except (AttributeError, ValueError, TypeError, IndexError):
-        fine = False
-    if not fine:
-        _check_rotate(rope, x, positions, out)
-    _check(load().aatc_rotate(rope._ref, _TYPES[dtype], x.data_ptr(), xs[0], xs[1], positions.data_ptr(), n, h,
-                              1 if backward else 0, out.data_ptr(), os[0], os[1], _stream(stream)), "aatc_rotate")
-    return out
-
-
-def _check_rotate(rope, x, positions, out):
     where = "aatc_rotate"
     if not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
     if not _on_device(x) or x.dtype not in _TYPES:
         _arg_error(where, "x must be a device tensor of torch.bfloat16 or torch.float16")
-    _heads(x, where, "x", None)
-    _heads(out, where, "out", x.dtype, x.shape[1], x.shape[0])
-    _ints(positions, where, "positions", x.shape[0])
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    st = _calls.rotate(rope._addr, _TYPES[x.dtype], x.dtype, x, positions, out, bool(backward),
+                       None if stream is None else stream.cuda_stream)
+    if st is None:
+        a = _heads(x, where, "x", None)
+        n, h = x.shape[0], x.shape[1]
+        b = _heads(out, where, "out", x.dtype, h, n)
+        st = load().aatc_rotate(rope._addr, _TYPES[x.dtype], a.x, a.token_stride, a.head_stride,
+                                _ints(positions, where, "positions", n), n, h, int(bool(backward)), b.x, b.token_stride,
+                                b.head_stride, _stream(stream))
+    if st:
+        _check(st, where)
+    return out
 
 
 def append(pages: Pages, layer: int, k, v, table, index, rows=None, positions=None, rope: Rotary | None = None, q=None,
@@ -203,74 +211,43 @@ def append(pages: Pages, layer: int, k, v, table, index, rows=None, positions=No
     keys turned by rope; index int32 [tokens] in the sequence (negative: padding, nothing is written),
     rows int32 [tokens] of the table (None: token t in row t), positions int32 [tokens] for the rotation
     (None: the index).  q [tokens][n_q_heads][128] is turned along; returns q_out (None without q)."""
-    dtype, n_q, qh, ro, op = pages.dtype, 0, None, None, None
-    try:
-        n, n_kv, d = k.shape
-        tn, tm = table.shape
-        one = (n,)
-        ks, vs, ts = k.stride(), v.stride(), table.stride()
-        fine = (d == HEAD_DIM and n_kv == pages.n_kv_heads and k.is_cuda and k.dtype is dtype and ks[2] == 1 and v.is_cuda and
-                v.dtype is dtype and v.shape == k.shape and vs[2] == 1 and table.is_cuda and table.dtype is _I32T and
-                (ts[1] == 1 or tm <= 1) and index.is_cuda and index.dtype is _I32T and index.shape == one and
-                index.is_contiguous())
-        if rows is None:
-            fine = fine and n <= tn
-        else:
-            fine = fine and rows.is_cuda and rows.dtype is _I32T and rows.shape == one and rows.is_contiguous()
-        if positions is not None:
-            fine = (fine and positions.is_cuda and positions.dtype is _I32T and positions.shape == one and
-                    positions.is_contiguous())
-        if q is not None:
-            n_q = q.shape[1]
-            if q_out is None:
-                q_out = torch.empty((n, n_q, HEAD_DIM), dtype=dtype, device=q.device)
-            qs = q.stride()
-            fine = (fine and rope is not None and q.is_cuda and q.dtype is dtype and q.shape == (n, n_q, HEAD_DIM) and
-                    qs[2] == 1 and (q_out is q or (q_out.is_cuda and q_out.dtype is dtype and q_out.shape == q.shape and
-                                                   q_out.is_contiguous())))
-            qh, op = ctypes.byref(_Heads(q.data_ptr(), qs[0], qs[1])), q_out.data_ptr()
-        elif q_out is not None:
-            fine = False
-        if rope is not None:
-            ro = rope._ref
-    except (AttributeError, ValueError, TypeError, IndexError):
-        fine = False
-    if not fine:
-        _check_append(pages, k, v, table, index, rows, positions, rope, q, q_out)
-    _check(pages._lib.aatc_paged_append(pages._ref, pages.layer(layer, "aatc_paged_append"), table.data_ptr(), tn,
-                                        ts[0] if tn > 1 else tm, tm, None if rows is None else rows.data_ptr(),
-                                        index.data_ptr(), None if positions is None else positions.data_ptr(), n,
-                                        ctypes.byref(_Heads(k.data_ptr(), ks[0], ks[1])),
-                                        ctypes.byref(_Heads(v.data_ptr(), vs[0], vs[1])), ro, qh, n_q, op, pages._flags,
-                                        _stream(stream)), "aatc_paged_append")
-    return q_out
-
-
-def _check_append(pages, k, v, table, index, rows, positions, rope, q, q_out):
-    where, dtype = "aatc_paged_append", pages.dtype
-    _heads(k, where, "k", dtype, pages.n_kv_heads)
-    n = k.shape[0]
-    _heads(v, where, "v", dtype, pages.n_kv_heads, n)
-    _table(table, where)
-    _ints(index, where, "index", n)
-    if rows is not None:
-        _ints(rows, where, "rows", n)
-    elif table.shape[0] < n:
-        _arg_error(where, f"table has {table.shape[0]} rows for {n} tokens: give rows")
-    if positions is not None:
-        _ints(positions, where, "positions", n)
+    where = "aatc_paged_append"
+    _pages(pages, where)
     if rope is not None and not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
-    if q is not None:
-        if rope is None:
-            _arg_error(where, "q without rope")
-        _heads(q, where, "q", dtype, None, n)
-        if q_out is not q:
-            _heads(q_out, where, "q_out", dtype, q.shape[1], n)
-            if not q_out.is_contiguous():
+    if q is not None and q_out is None and _on_device(q):
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    base, ro = pages.layer(layer, where), None if rope is None else rope._addr
+    st = _calls.append(pages._addr, base, pages._flags, pages.dtype, pages.n_kv_heads, k, v, table, index, rows, positions, ro,
+                       q, q_out, None if stream is None else stream.cuda_stream)
+    if st is None:
+        dtype = pages.dtype
+        kh = _heads(k, where, "k", dtype, pages.n_kv_heads)
+        n = k.shape[0]
+        vh = _heads(v, where, "v", dtype, pages.n_kv_heads, n)
+        tp, tn, ts, tm = _table(table, where)
+        ip = _ints(index, where, "index", n)
+        rp = None if rows is None else _ints(rows, where, "rows", n)
+        if rows is None and tn < n:
+            _arg_error(where, f"table has {tn} rows for {n} tokens: give rows")
+        pp = None if positions is None else _ints(positions, where, "positions", n)
+        qh, n_q, op = None, 0, None
+        if q is not None:
+            if rope is None:
+                _arg_error(where, "q without rope")
+            qh = _heads(q, where, "q", dtype, None, n)
+            n_q = q.shape[1]
+            op = q_out.data_ptr() if q_out is q else _heads(q_out, where, "q_out", dtype, n_q, n).x
+            if q_out is not q and not q_out.is_contiguous():
                 _arg_error(where, "q_out must be contiguous, or q itself")
-    elif q_out is not None:
-        _arg_error(where, "q_out without q")
+            qh = ctypes.byref(qh)
+        elif q_out is not None:
+            _arg_error(where, "q_out without q")
+        st = pages._lib.aatc_paged_append(pages._addr, base, tp, tn, ts, tm, rp, ip, pp, n, ctypes.byref(kh),
+                                          ctypes.byref(vh), ro, qh, n_q, op, pages._flags, _stream(stream))
+    if st:
+        _check(st, where)
+    return q_out
 
 
 def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=None, prior=None, scale: float | None = None,
@@ -280,122 +257,92 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
     [batch][n_q_heads], written; prior: (out, lse) of another set of tokens that joins the softmax; scale:
     1 / sqrt(128) by default; cap: scores become cap tanh(score / cap); window: only the last ones; slopes:
     fp32 [n_q_heads], slope (t - (len - 1)) is added to the score of token t."""
-    try:
-        batch, n_q, d = q.shape
-        tn, tm = table.shape
-        if out is None:
-            out = torch.empty((batch, n_q, HEAD_DIM), dtype=_F32T, device=q.device)
-        qs, ts = q.stride(), table.stride()
-        fine = (d == HEAD_DIM and q.is_cuda and q.dtype is pages.dtype and qs[2] == 1 and table.is_cuda and
-                table.dtype is _I32T and tn == batch and (ts[1] == 1 or tm <= 1) and lens.is_cuda and lens.dtype is _I32T and
-                lens.shape == (batch,) and lens.is_contiguous() and out.is_cuda and out.dtype is _F32T and
-                out.shape == q.shape and out.is_contiguous() and
-                (workspace is None or (workspace.is_cuda and workspace.is_contiguous())))
-        how = _Decode(0.08838834764831845 if scale is None else scale, cap, window)
-        ep = None
-        if lse is not None:
-            fine = fine and lse.is_cuda and lse.dtype is _F32T and lse.shape == (batch, n_q) and lse.is_contiguous()
-            ep = lse.data_ptr()
-        if slopes is not None:
-            fine = fine and slopes.is_cuda and slopes.dtype is _F32T and slopes.shape == (n_q,) and slopes.is_contiguous()
-            how.slopes = slopes.data_ptr()
-        if prior is not None:
-            po, pl = prior
-            fine = (fine and po.is_cuda and po.dtype is _F32T and po.shape == q.shape and po.is_contiguous() and pl.is_cuda and
-                    pl.dtype is _F32T and pl.shape == (batch, n_q) and pl.is_contiguous())
-            how.prior_out, how.prior_lse = po.data_ptr(), pl.data_ptr()
-    except (AttributeError, ValueError, TypeError, IndexError):
-        fine = False
-    if not fine:
-        _check_decode(pages, q, table, lens, out, lse, prior, slopes, workspace)
-    base = pages.layer(layer, "aatc_paged_decode_attention")
-    if batch == 0:
-        return out
-    if workspace is None:                 # (the library refuses one that is too small)
-        workspace = pages.decode_workspace(n_q)
-    _check(pages._lib.aatc_paged_decode_attention(pages._ref, base, table.data_ptr(), ts[0] if tn > 1 else tm, tm,
-                                                  lens.data_ptr(), batch, ctypes.byref(_Heads(q.data_ptr(), qs[0], qs[1])),
-                                                  n_q, ctypes.byref(how), out.data_ptr(), ep, workspace.data_ptr(),
-                                                  workspace.nbytes, pages._flags, _stream(stream)),
-           "aatc_paged_decode_attention")
-    return out
-
-
-def _check_decode(pages, q, table, lens, out, lse, prior, slopes, workspace):
     where = "aatc_paged_decode_attention"
-    _heads(q, where, "q", pages.dtype)
-    batch, n_q = q.shape[0], q.shape[1]
-    _table(table, where, batch)
-    _ints(lens, where, "lens", batch)
-    _floats(out, where, "out", (batch, n_q, HEAD_DIM))
-    if lse is not None:
-        _floats(lse, where, "lse", (batch, n_q))
-    if slopes is not None:
-        _floats(slopes, where, "slopes", (n_q,))
-    if prior is not None:
-        if not isinstance(prior, (tuple, list)) or len(prior) != 2:
-            _arg_error(where, "prior must be (out, lse)")
-        _floats(prior[0], where, "prior[0]", (batch, n_q, HEAD_DIM))
-        _floats(prior[1], where, "prior[1]", (batch, n_q))
-    if workspace is not None and (not _on_device(workspace) or not workspace.is_contiguous()):
-        _arg_error(where, "workspace must be a contiguous device tensor")
+    _pages(pages, where)
+    base = pages.layer(layer, where)
+    if out is None and _on_device(q):
+        out = torch.empty(q.shape, dtype=_F32T, device=q.device)
+    if prior is None:
+        prior = (None, None)
+    elif not isinstance(prior, (tuple, list)) or len(prior) != 2 or prior[0] is None or prior[1] is None:
+        _arg_error(where, "prior must be (out, lse)")
+    if scale is None:
+        scale = 0.08838834764831845       # 1 / sqrt(128)
+    st = None
+    if workspace is not None:
+        st = _calls.decode(pages._addr, base, pages._flags, pages.dtype, q, table, lens, out, lse, prior[0], prior[1], scale,
+                           cap, window, slopes, workspace, None if stream is None else stream.cuda_stream)
+    if st is None:
+        qh = _heads(q, where, "q", pages.dtype)
+        batch, n_q = q.shape[0], q.shape[1]
+        tp, _, ts, tm = _table(table, where, batch)
+        lp = _ints(lens, where, "lens", batch)
+        op = _floats(out, where, "out", (batch, n_q, HEAD_DIM))
+        ep = None if lse is None else _floats(lse, where, "lse", (batch, n_q))
+        how = _Decode(scale, cap, window)
+        if slopes is not None:
+            how.slopes = _floats(slopes, where, "slopes", (n_q,))
+        if prior[0] is not None:
+            how.prior_out = _floats(prior[0], where, "prior[0]", (batch, n_q, HEAD_DIM))
+            how.prior_lse = _floats(prior[1], where, "prior[1]", (batch, n_q))
+        if batch == 0:
+            return out
+        if workspace is None:             # (the library refuses one that is too small)
+            workspace = pages.decode_workspace(n_q)
+        elif not _on_device(workspace) or not workspace.is_contiguous():
+            _arg_error(where, "workspace must be a contiguous device tensor")
+        st = pages._lib.aatc_paged_decode_attention(pages._addr, base, tp, ts, tm, lp, batch, ctypes.byref(qh), n_q,
+                                                    ctypes.byref(how), op, ep, workspace.data_ptr(), workspace.nbytes,
+                                                    pages._flags, _stream(stream))
+    if st:
+        _check(st, where)
+    return out
 
 
 def copy_pages(pages: Pages, pairs, stream=None):
     """aatc_pages_copy: page pairs[i][0] to page pairs[i][1] in every layer; pairs int32 [n][2] on the
     host.  No page may be written twice, or be both read and written."""
+    where = "aatc_pages_copy"
+    _pages(pages, where)
     p = pairs
     if not isinstance(p, np.ndarray) or p.dtype != np.int32 or not p.flags.c_contiguous:
         p = np.ascontiguousarray(pairs, dtype=np.int32)
     if p.size == 0:
         return
     if p.ndim != 2 or p.shape[1] != 2:
-        _arg_error("aatc_pages_copy", "pairs must be [n][2]")
-    _check(pages._lib.aatc_pages_copy(pages._ref, pages._layers[0], pages.n_layers, pages.layer_bytes,
-                                      p.__array_interface__["data"][0], p.shape[0], _stream(stream)), "aatc_pages_copy")
+        _arg_error(where, "pairs must be [n][2]")
+    _check(pages._lib.aatc_pages_copy(pages._addr, pages._layers[0], pages.n_layers, pages.layer_bytes,
+                                      p.__array_interface__["data"][0], p.shape[0], _stream(stream)), where)
 
 
 def gather(pages: Pages, layer: int, table, first: int, n_tokens: int, lens=None, out=None, stream=None):
     """aatc_paged_gather: tokens [first, first + n_tokens) of every row of the table, contiguous:
     (K, V), each [rows][n_tokens][n_kv_heads][128] as aatc_encode takes them.  lens: int32 [rows];
     tokens past their sequence's length come out as zeros."""
-    try:
-        tn, tm = table.shape
-        ts, dtype = table.stride(), pages.dtype
-        shape = (tn, n_tokens, pages.n_kv_heads, HEAD_DIM)
-        fine = table.is_cuda and table.dtype is _I32T and (ts[1] == 1 or tm <= 1) and n_tokens >= 0
-        if out is not None:
-            k, v = out
-            fine = (fine and k.is_cuda and k.dtype is dtype and k.shape == shape and k.is_contiguous() and v.is_cuda and
-                    v.dtype is dtype and v.shape == shape and v.is_contiguous())
-        elif fine:
-            k, v = pages.data.new_empty(shape), pages.data.new_empty(shape)
-        if lens is not None:
-            fine = fine and lens.is_cuda and lens.dtype is _I32T and lens.shape == (tn,) and lens.is_contiguous()
-    except (AttributeError, ValueError, TypeError, IndexError):
-        fine = False
-    if not fine:
-        k, v = _check_gather(pages, table, n_tokens, lens, out)
-    _check(pages._lib.aatc_paged_gather(pages._ref, pages.layer(layer, "aatc_paged_gather"), table.data_ptr(), tn,
-                                        ts[0] if tn > 1 else tm, tm, first, n_tokens,
-                                        None if lens is None else lens.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                        pages._flags, _stream(stream)), "aatc_paged_gather")
-    return k, v
-
-
-def _check_gather(pages, table, n_tokens, lens, out):
     where = "aatc_paged_gather"
-    _table(table, where)
-    shape = (table.shape[0], n_tokens, pages.n_kv_heads, HEAD_DIM)
-    if n_tokens < 0:
-        _arg_error(where, "n_tokens must not be negative")
+    _pages(pages, where)
+    base = pages.layer(layer, where)
     if out is None:
-        out = pages.data.new_empty(shape), pages.data.new_empty(shape)
-    if not isinstance(out, (tuple, list)) or len(out) != 2:
+        _table(table, where)
+        if n_tokens < 0:
+            _arg_error(where, "n_tokens must not be negative")
+        shape = (table.shape[0], n_tokens, pages.n_kv_heads, HEAD_DIM)
+        k, v = pages.data.new_empty(shape), pages.data.new_empty(shape)
+    elif isinstance(out, (tuple, list)) and len(out) == 2:
+        k, v = out
+    else:
         _arg_error(where, "out must be (K, V)")
-    for t in out:
-        if not _on_device(t) or t.dtype != pages.dtype or t.shape != shape or not t.is_contiguous():
-            _arg_error(where, f"out must be two contiguous device tensors of the pages' type, {shape}")
-    if lens is not None:
-        _ints(lens, where, "lens", table.shape[0])
-    return out
+    st = _calls.gather(pages._addr, base, pages._flags, pages.dtype, pages.n_kv_heads, table, first, n_tokens, lens, k, v,
+                       None if stream is None else stream.cuda_stream)
+    if st is None:
+        tp, tn, ts, tm = _table(table, where)
+        shape = (tn, int(n_tokens), pages.n_kv_heads, HEAD_DIM)
+        for t in (k, v):
+            if not _on_device(t) or t.dtype != pages.dtype or t.shape != shape or not t.is_contiguous():
+                _arg_error(where, f"out must be two contiguous device tensors of the pages' type, {shape}")
+        lp = None if lens is None else _ints(lens, where, "lens", tn)
+        st = pages._lib.aatc_paged_gather(pages._addr, base, tp, tn, ts, tm, int(first), int(n_tokens), lp, k.data_ptr(),
+                                          v.data_ptr(), pages._flags, _stream(stream))
+    if st:
+        _check(st, where)
+    return k, v
