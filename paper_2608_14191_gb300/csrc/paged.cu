@@ -50,71 +50,83 @@ __device__ __forceinline__ float2 cos_sin(const Turn& t, int32_t position, uint6
 
 // A head is eight units of sixteen dimensions, two 16-byte pieces each: of the rotated part, pieces whose
 // values pair up (half layout: rot_dim / 2 apart; interleaved: side by side), eight pairs with
-// the frequencies 8 u .. 8 u + 7; of the rest, two neighbouring pieces.
+// the frequencies 8 u .. 8 u + 7; of the rest, two neighbouring pieces.  A thread takes unit u of kHeads heads of a
+// token: all its loads first, then (while they are under way) the eight sines and cosines, which serve
+// all its heads.  Memory is the bound where there are many tokens, and latency where there are few, which is what
+// one head a thread is for.
 constexpr int kUnits = 8;
+constexpr int kManyHeads = 4;
+constexpr int64_t kFewRows = 16384; // tokens x heads up to which a thread takes one head
 
-template <typename T>
-__device__ __forceinline__ void rotate_unit(const Turn& t, int u, int32_t position, const T* x, T* out) {
-  const bool turned = 16 * u < t.rot_dim;
-  const int a = turned && !t.interleaved ? 8 * u : 16 * u;
-  const int b = turned && !t.interleaved ? 8 * u + t.rot_dim / 2 : 16 * u + 8;
-  uint4 pa = *reinterpret_cast<const uint4*>(x + a), pb = *reinterpret_cast<const uint4*>(x + b);
-  if (turned) {
-    uint32_t* wa = reinterpret_cast<uint32_t*>(&pa);
-    uint32_t* wb = reinterpret_cast<uint32_t*>(&pb);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 e0 = cos_sin(t, position, t.turns[8 * u + (t.interleaved ? i : 2 * i)]);
-      const float2 e1 = cos_sin(t, position, t.turns[8 * u + (t.interleaved ? i + 4 : 2 * i + 1)]);
-      const float2 va = widen(T(), wa[i]), vb = widen(T(), wb[i]);
-      if (t.interleaved) {
-        wa[i] = narrow(T(), va.x * e0.x - va.y * e0.y, va.x * e0.y + va.y * e0.x);
-        wb[i] = narrow(T(), vb.x * e1.x - vb.y * e1.y, vb.x * e1.y + vb.y * e1.x);
-      } else {
-        wa[i] = narrow(T(), va.x * e0.x - vb.x * e0.y, va.y * e1.x - vb.y * e1.y);
-        wb[i] = narrow(T(), va.x * e0.y + vb.x * e0.x, va.y * e1.y + vb.y * e1.x);
-      }
-    }
-  }
-  *reinterpret_cast<uint4*>(out + a) = pa;
-  *reinterpret_cast<uint4*>(out + b) = pb;
-}
-
-// One CTA per token.
-template <typename T>
-__global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs a) {
-  const int64_t t = blockIdx.x;
+template <typename T, int kHeads>
+__global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs a, int groups) {
+  const Pool& p = a.pool;
+  const int n_heads = a.n_q + (p.pages ? 2 * p.n_kv : 0);
+  const int64_t job = static_cast<int64_t>(blockIdx.x) * (256 / kUnits) + threadIdx.x / kUnits;
+  const int64_t t = job / groups;
+  const int group = static_cast<int>(job - t * groups), u = threadIdx.x % kUnits;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  if (t >= a.n_tokens) return;
+  const int rot = a.turn.turns ? a.turn.rot_dim : 0;
+  const bool turned = 16 * u < rot, apart = turned && !a.turn.interleaved;
+  const int off_a = 2 * (apart ? 8 * u : 16 * u), off_b = 2 * (apart ? 8 * u + rot / 2 : 16 * u + 8);   // bytes
   const int32_t index = a.index[t];
   const int32_t position = a.positions ? a.positions[t] : index;
-  const T* q = static_cast<const T*>(a.q.x) + t * a.q.token_stride;
-  T* qo = static_cast<T*>(a.q_out) + t * a.q_out_token_stride;
-  for (int i = threadIdx.x; i < a.n_q * kUnits; i += blockDim.x)
-    rotate_unit(a.turn, i % kUnits, position, q + (i / kUnits) * a.q.head_stride,
-                qo + (i / kUnits) * a.q_out_head_stride);
-  const Pool& p = a.pool;
-  if (!p.pages || index < 0) return;
   const int64_t row = a.rows ? a.rows[t] : t;
-  if (row < 0 || row >= a.n_rows || (index >> p.page_shift) >= p.max_pages) {
-    raise(p.err, kBadRow);
-    return;
+  uint4 x[kHeads][2];
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) {
+    const int h = group + i * groups;
+    if (h >= n_heads) break;
+    const Heads& from = h < a.n_q ? a.q : h < a.n_q + p.n_kv ? a.k : a.v;
+    const int in = h < a.n_q ? h : h < a.n_q + p.n_kv ? h - a.n_q : h - a.n_q - p.n_kv;
+    const char* src = static_cast<const char*>(from.x) + 2 * (t * from.token_stride + in * from.head_stride);
+    x[i][0] = *reinterpret_cast<const uint4*>(src + off_a);
+    x[i][1] = *reinterpret_cast<const uint4*>(src + off_b);
   }
-  const int32_t id = p.table[row * p.table_stride + (index >> p.page_shift)];
-  if (id < 0 || id >= p.n_pages) {
-    raise(p.err, kBadPage);
-    return;
+  // the token's place: keys of all heads of a page, then values; head h of kind c is block (2 id + c) n_kv + h
+  char* place = nullptr;
+  if (p.pages && index >= 0 && group + (kHeads - 1) * groups >= a.n_q) {
+    if (row < 0 || row >= a.n_rows || (index >> p.page_shift) >= p.max_pages) {
+      raise(p.err, kBadRow);
+    } else {
+      const int32_t id = __ldg(p.table + row * p.table_stride + (index >> p.page_shift));
+      if (id < 0 || id >= p.n_pages) raise(p.err, kBadPage);
+      else
+        place = static_cast<char*>(p.pages) + ((static_cast<int64_t>(id) * 2 * p.n_kv << p.page_shift) +
+                                               (index & ((1 << p.page_shift) - 1))) * (2 * D);
+    }
   }
-  // keys of all heads of a page, then values: head h of kind c at block (2 id + c) n_kv + h
-  T* page = static_cast<T*>(p.pages) + ((static_cast<int64_t>(id) * 2 * p.n_kv << p.page_shift) +
-                                        (index & ((1 << p.page_shift) - 1))) * D;
-  const T* k = static_cast<const T*>(a.k.x) + t * a.k.token_stride;
-  const T* v = static_cast<const T*>(a.v.x) + t * a.v.token_stride;
-  Turn none = a.turn;
-  none.rot_dim = 0;
-  for (int i = threadIdx.x; i < 2 * p.n_kv * kUnits; i += blockDim.x) {
-    const int h = i / kUnits;
-    T* to = page + (static_cast<int64_t>(h) << p.page_shift) * D;
-    if (h < p.n_kv) rotate_unit(a.turn.turns ? a.turn : none, i % kUnits, position, k + h * a.k.head_stride, to);
-    else rotate_unit(none, i % kUnits, position, v + (h - p.n_kv) * a.v.head_stride, to);
+  float2 e[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = turned ? cos_sin(a.turn, position, __ldg(a.turn.turns + 8 * u + i)) : make_float2(1.0f, 0.0f);
+#pragma unroll
+  for (int i = 0; i < kHeads; ++i) {
+    const int h = group + i * groups;
+    if (h >= n_heads) break;
+    if (turned && h < a.n_q + p.n_kv) {
+      uint32_t* wa = reinterpret_cast<uint32_t*>(&x[i][0]);
+      uint32_t* wb = reinterpret_cast<uint32_t*>(&x[i][1]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 va = widen(T(), wa[j]), vb = widen(T(), wb[j]);
+        if (a.turn.interleaved) {
+          wa[j] = narrow(T(), va.x * e[j].x - va.y * e[j].y, va.x * e[j].y + va.y * e[j].x);
+          wb[j] = narrow(T(), vb.x * e[4 + j].x - vb.y * e[4 + j].y, vb.x * e[4 + j].y + vb.y * e[4 + j].x);
+        } else {
+          const float2 e0 = e[2 * j], e1 = e[2 * j + 1];
+          wa[j] = narrow(T(), va.x * e0.x - vb.x * e0.y, va.y * e1.x - vb.y * e1.y);
+          wb[j] = narrow(T(), va.x * e0.y + vb.x * e0.x, va.y * e1.y + vb.y * e1.x);
+        }
+      }
+    }
+    char* dst;
+    if (h < a.n_q) dst = static_cast<char*>(a.q_out) + 2 * (t * a.q_out_token_stride + h * a.q_out_head_stride);
+    else if (place) dst = place + (static_cast<int64_t>(h - a.n_q) << p.page_shift) * (2 * D);
+    else continue;
+    *reinterpret_cast<uint4*>(dst + off_a) = x[i][0];
+    *reinterpret_cast<uint4*>(dst + off_b) = x[i][1];
   }
 }
 
@@ -827,47 +839,82 @@ __global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const 
 }
 
 // ---------------------------------------------------------------- page copies
+constexpr int kCopyVecs = 4;        // 16-byte pieces of a thread, all loaded before the first is stored
+
+// One CTA per 16 KB of a page (blockIdx.x), pair and layer.
 template <int N>
 __global__ void __launch_bounds__(256) aatc_pages_copy_kernel(uint4* pages, int64_t page_vecs, int64_t layer_vecs,
                                                               const __grid_constant__ CopyPairs<N> pairs) {
-  const int2 pr = pairs.pair[blockIdx.x];
-  const uint4* src = pages + blockIdx.y * layer_vecs + pr.x * page_vecs;
-  uint4* dst = pages + blockIdx.y * layer_vecs + pr.y * page_vecs;
-  for (int64_t i = threadIdx.x; i < page_vecs; i += blockDim.x) dst[i] = src[i];
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int2 pr = pairs.pair[blockIdx.y];
+  const uint4* src = pages + blockIdx.z * layer_vecs + pr.x * page_vecs;
+  uint4* dst = pages + blockIdx.z * layer_vecs + pr.y * page_vecs;
+  const int64_t i0 = static_cast<int64_t>(blockIdx.x) * (256 * kCopyVecs) + threadIdx.x;
+  uint4 x[kCopyVecs];
+#pragma unroll
+  for (int k = 0; k < kCopyVecs; ++k)
+    if (i0 + 256 * k < page_vecs) x[k] = src[i0 + 256 * k];
+#pragma unroll
+  for (int k = 0; k < kCopyVecs; ++k)
+    if (i0 + 256 * k < page_vecs) dst[i0 + 256 * k] = x[k];
 }
 
 // ---------------------------------------------------------------- gather
-// One CTA per token: the keys of all kv-heads, then the values.
+// A token's row is the keys of all kv-heads, then the values; one CTA per 16 KB of a sequence's rows, four pieces a
+// thread, all loaded before the first is stored.
 __global__ void __launch_bounds__(256) aatc_paged_gather_kernel(const GatherArgs a) {
-  const Pool& p = a.pool;
-  const int r = blockIdx.y, t = a.first + blockIdx.x;
-  bool seen = !a.lens || t < a.lens[r];
-  int32_t id = 0;
-  if (seen) {
-    id = p.table[static_cast<int64_t>(r) * p.table_stride + (t >> p.page_shift)];
-    if (id < 0 || id >= p.n_pages) {
-      if (threadIdx.x == 0) raise(p.err, kBadPage);
-      seen = false;
-    }
-  }
   constexpr int kVecs = D / 8;                                 // 16-byte pieces of a head
-  const uint4* page = static_cast<const uint4*>(p.pages) +
-                      ((static_cast<int64_t>(id) * 2 * p.n_kv << p.page_shift) + (t & ((1 << p.page_shift) - 1))) * kVecs;
-  const int64_t to = (static_cast<int64_t>(r) * a.n_tokens + blockIdx.x) * p.n_kv;
-  for (int i = threadIdx.x; i < 2 * p.n_kv * kVecs; i += blockDim.x) {
-    const int h = i / kVecs, c = i % kVecs;
-    const uint4 x = seen ? page[(static_cast<int64_t>(h) << p.page_shift) * kVecs + c] : make_uint4(0, 0, 0, 0);
-    uint4* out = static_cast<uint4*>(h < p.n_kv ? a.k_out : a.v_out);
-    out[(to + (h < p.n_kv ? h : h - p.n_kv)) * kVecs + c] = x;
+  const Pool& p = a.pool;
+  const uint32_t row_vecs = 2 * p.n_kv * kVecs;
+  const int r = blockIdx.y;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  const int n = a.lens ? __ldg(a.lens + r) : INT32_MAX;
+  const int32_t* row = p.table + static_cast<int64_t>(r) * p.table_stride;
+  uint4 x[kCopyVecs];
+  uint4* to[kCopyVecs];
+#pragma unroll
+  for (int k = 0; k < kCopyVecs; ++k) {
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * kCopyVecs + k) * 256 + threadIdx.x;
+    const int64_t i_tok = i >> 32 ? i / row_vecs : static_cast<uint32_t>(i) / row_vecs;
+    to[k] = nullptr;
+    if (i_tok >= a.n_tokens) continue;
+    const int c = static_cast<int>(i - i_tok * row_vecs), h = c / kVecs, t = a.first + static_cast<int>(i_tok);
+    const bool key = h < p.n_kv;
+    to[k] = static_cast<uint4*>(key ? a.k_out : a.v_out) +
+            ((static_cast<int64_t>(r) * a.n_tokens + i_tok) * p.n_kv + (key ? h : h - p.n_kv)) * kVecs + c % kVecs;
+    x[k] = make_uint4(0, 0, 0, 0);
+    if (t >= n) continue;
+    const int32_t id = __ldg(row + (t >> p.page_shift));
+    if (id < 0 || id >= p.n_pages) {
+      raise(p.err, kBadPage);
+      continue;
+    }
+    x[k] = static_cast<const uint4*>(p.pages)[(((static_cast<int64_t>(id) * 2 * p.n_kv + h) << p.page_shift) +
+                                               (t & ((1 << p.page_shift) - 1))) * kVecs + c % kVecs];
   }
+#pragma unroll
+  for (int k = 0; k < kCopyVecs; ++k)
+    if (to[k]) *to[k] = x[k];
 }
 
 }  // namespace
 
+template <typename T, int kHeads>
+static cudaError_t launch_append_t(const AppendArgs& a, int n_heads, cudaStream_t st) {
+  const int groups = (n_heads + kHeads - 1) / kHeads;
+  const int64_t blocks = (static_cast<int64_t>(a.n_tokens) * groups + 256 / kUnits - 1) / (256 / kUnits);
+  if (blocks > INT32_MAX) return cudaErrorNotSupported;
+  return launch_pdl(aatc_paged_append_kernel<T, kHeads>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a, groups);
+}
+
 cudaError_t launch_append(int dtype, const AppendArgs& a, cudaStream_t st) {
-  if (dtype == AATC_BF16) aatc_paged_append_kernel<__nv_bfloat16><<<a.n_tokens, 256, 0, st>>>(a);
-  else aatc_paged_append_kernel<__half><<<a.n_tokens, 256, 0, st>>>(a);
-  return cudaGetLastError();
+  const int n_heads = a.n_q + (a.pool.pages ? 2 * a.pool.n_kv : 0);
+  const bool few = static_cast<int64_t>(a.n_tokens) * n_heads <= kFewRows;
+  if (dtype == AATC_BF16)
+    return few ? launch_append_t<__nv_bfloat16, 1>(a, n_heads, st) : launch_append_t<__nv_bfloat16, kManyHeads>(a, n_heads, st);
+  return few ? launch_append_t<__half, 1>(a, n_heads, st) : launch_append_t<__half, kManyHeads>(a, n_heads, st);
 }
 
 size_t decode_workspace(int num_sms) {
@@ -889,16 +936,24 @@ cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
   return launch_pdl(aatc_paged_join_kernel, dim3(ctas, std::min(a.group, kSegHeads)), dim3(kJoinWarps * 32), 0, st, a, ctas);
 }
 
+template <int N>
+static cudaError_t launch_copy_n(void* pages, size_t page_bytes, int n_layers, size_t layer_stride, const int32_t* pairs,
+                                 int n, cudaStream_t st) {
+  CopyPairs<N> cp;
+  for (int i = 0; i < n; ++i) cp.pair[i] = make_int2(pairs[2 * i], pairs[2 * i + 1]);
+  const int64_t vecs = static_cast<int64_t>(page_bytes / 16);
+  const dim3 grid(static_cast<unsigned>((vecs + 256 * kCopyVecs - 1) / (256 * kCopyVecs)), n, n_layers);
+  return launch_pdl(aatc_pages_copy_kernel<N>, grid, dim3(256), 0, st, static_cast<uint4*>(pages), vecs,
+                    static_cast<int64_t>(layer_stride / 16), cp);
+}
+
 cudaError_t launch_copy(void* pages, size_t page_bytes, int n_layers, size_t layer_stride, const int32_t* pairs,
                         int n_pairs, cudaStream_t st) {
-  constexpr int kMost = 500;                                   // pairs of a launch: 4000 bytes of parameters
+  constexpr int kMost = 500, kFew = 30;                        // pairs of a launch: 4000 bytes of parameters, or 240
   for (int i0 = 0; i0 < n_pairs; i0 += kMost) {
-    CopyPairs<kMost> cp;
     const int n = std::min(kMost, n_pairs - i0);
-    for (int i = 0; i < n; ++i) cp.pair[i] = make_int2(pairs[2 * (i0 + i)], pairs[2 * (i0 + i) + 1]);
-    aatc_pages_copy_kernel<kMost><<<dim3(n, n_layers), 256, 0, st>>>(static_cast<uint4*>(pages), page_bytes / 16,
-                                                                     layer_stride / 16, cp);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = (n <= kFew ? launch_copy_n<kFew> : launch_copy_n<kMost>)(pages, page_bytes, n_layers, layer_stride,
+                                                                                  pairs + 2 * i0, n, st);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -913,8 +968,10 @@ cudaError_t launch_gather(const GatherArgs& a, cudaStream_t st) {
     const size_t skip = static_cast<size_t>(r0) * a.n_tokens * a.pool.n_kv * D * 2;
     s.k_out = static_cast<char*>(a.k_out) + skip;
     s.v_out = static_cast<char*>(a.v_out) + skip;
-    aatc_paged_gather_kernel<<<dim3(a.n_tokens, s.n_rows), 256, 0, st>>>(s);
-    const cudaError_t e = cudaGetLastError();
+    const int64_t vecs = static_cast<int64_t>(a.n_tokens) * a.pool.n_kv * (2 * D / 8);
+    const int64_t blocks = (vecs + 256 * kCopyVecs - 1) / (256 * kCopyVecs);
+    if (blocks > INT32_MAX) return cudaErrorNotSupported;
+    const cudaError_t e = launch_pdl(aatc_paged_gather_kernel, dim3(static_cast<unsigned>(blocks), s.n_rows), dim3(256), 0, st, s);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

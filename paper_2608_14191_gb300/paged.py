@@ -323,11 +323,11 @@ def gather(pages: Pages, layer: int, table, first: int, n_tokens: int, lens=None
     _pages(pages, where)
     base = pages.layer(layer, where)
     if out is None:
-        _table(table, where)
-        if n_tokens < 0:
-            _arg_error(where, "n_tokens must not be negative")
+        if not _on_device(table) or n_tokens < 0:
+            _arg_error(where, "table must be a device tensor, n_tokens not negative")
         shape = (table.shape[0], n_tokens, pages.n_kv_heads, HEAD_DIM)
-        k, v = pages.data.new_empty(shape), pages.data.new_empty(shape)
+        k = torch.empty(shape, dtype=pages.dtype, device=pages.device)
+        v = torch.empty(shape, dtype=pages.dtype, device=pages.device)
     elif isinstance(out, (tuple, list)) and len(out) == 2:
         k, v = out
     else:
