@@ -51,34 +51,34 @@ __device__ __forceinline__ float2 cos_sin(const Turn& t, int32_t position, uint6
 // A head is eight units of sixteen dimensions, two 16-byte pieces each: of the rotated part, pieces whose
 // values pair up (half layout: rot_dim / 2 apart; interleaved: side by side), eight pairs with
 // the frequencies 8 u .. 8 u + 7; of the rest, two neighbouring pieces.  A thread takes unit u of kHeads heads of a
-// token: all its loads first, then (while they are under way) the eight sines and cosines, which serve
-// all its heads.  Memory is the bound where there are many tokens, and latency where there are few, which is what
+// token: all its loads first; while they are under way the CTA makes the sines and cosines of its tokens, each
+// once.  Memory is the bound where there are many tokens, and latency where there are few, which is what
 // one head a thread is for.
 constexpr int kUnits = 8;
+constexpr int kJobs = 256 / kUnits; // (token, group of heads) pairs of a CTA
 constexpr int kManyHeads = 4;
 constexpr int64_t kFewRows = 16384; // tokens x heads up to which a thread takes one head
 
 template <typename T, int kHeads>
 __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs a, int groups) {
+  // (cos, sin) of pairs 8 u + 2 j, 8 u + 2 j + 1 of a token at [j][u]: neighbouring units read neighbouring 16 bytes
+  __shared__ float4 s_turn[kJobs][4][kUnits];
   const Pool& p = a.pool;
   const int n_heads = a.n_q + (p.pages ? 2 * p.n_kv : 0);
-  const int64_t job = static_cast<int64_t>(blockIdx.x) * (256 / kUnits) + threadIdx.x / kUnits;
-  const int64_t t = job / groups;
+  const int64_t job0 = static_cast<int64_t>(blockIdx.x) * kJobs, job = job0 + threadIdx.x / kUnits;
+  const int64_t t0 = job0 / groups, t = job / groups;
   const int group = static_cast<int>(job - t * groups), u = threadIdx.x % kUnits;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  if (t >= a.n_tokens) return;
   const int rot = a.turn.turns ? a.turn.rot_dim : 0;
   const bool turned = 16 * u < rot, apart = turned && !a.turn.interleaved;
   const int off_a = 2 * (apart ? 8 * u : 16 * u), off_b = 2 * (apart ? 8 * u + rot / 2 : 16 * u + 8);   // bytes
-  const int32_t index = a.index[t];
-  const int32_t position = a.positions ? a.positions[t] : index;
-  const int64_t row = a.rows ? a.rows[t] : t;
+  const bool in_range = t < a.n_tokens;
   uint4 x[kHeads][2];
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) {
     const int h = group + i * groups;
-    if (h >= n_heads) break;
+    if (h >= n_heads || !in_range) break;
     const Heads& from = h < a.n_q ? a.q : h < a.n_q + p.n_kv ? a.k : a.v;
     const int in = h < a.n_q ? h : h < a.n_q + p.n_kv ? h - a.n_q : h - a.n_q - p.n_kv;
     const char* src = static_cast<const char*>(from.x) + 2 * (t * from.token_stride + in * from.head_stride);
@@ -87,7 +87,9 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
   }
   // the token's place: keys of all heads of a page, then values; head h of kind c is block (2 id + c) n_kv + h
   char* place = nullptr;
-  if (p.pages && index >= 0 && group + (kHeads - 1) * groups >= a.n_q) {
+  const int32_t index = p.pages && in_range ? __ldg(a.index + t) : -1;
+  if (index >= 0 && group + (kHeads - 1) * groups >= a.n_q) {
+    const int64_t row = a.rows ? __ldg(a.rows + t) : t;
     if (row < 0 || row >= a.n_rows || (index >> p.page_shift) >= p.max_pages) {
       raise(p.err, kBadRow);
     } else {
@@ -98,9 +100,25 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
                                                (index & ((1 << p.page_shift) - 1))) * (2 * D);
     }
   }
+  if (rot > 0) {
+    const int pairs = rot / 2, n = static_cast<int>(min((job0 + kJobs - 1) / groups, static_cast<int64_t>(a.n_tokens) - 1) - t0) + 1;
+    const int32_t* positions = (a.positions ? a.positions : a.index) + t0;
+    for (int i = threadIdx.x; i < n * pairs; i += 256) {
+      const int k = i / pairs, w = i - k * pairs;
+      reinterpret_cast<float2*>(&s_turn[k][w / 2 % 4][w / 8])[w % 2] = cos_sin(a.turn, __ldg(positions + k), __ldg(a.turn.turns + w));
+    }
+    __syncthreads();
+  }
+  if (!in_range) return;
   float2 e[8];
+  if (turned) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = turned ? cos_sin(a.turn, position, __ldg(a.turn.turns + 8 * u + i)) : make_float2(1.0f, 0.0f);
+    for (int j = 0; j < 4; ++j) {
+      const float4 two = s_turn[static_cast<int>(t - t0)][j][u];
+      e[2 * j] = make_float2(two.x, two.y);
+      e[2 * j + 1] = make_float2(two.z, two.w);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) {
     const int h = group + i * groups;
