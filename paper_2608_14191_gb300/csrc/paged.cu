@@ -37,6 +37,11 @@ __device__ __forceinline__ void raise(int32_t* err, int32_t bits) {
   if (err) atomicOr(err, bits);
 }
 
+// a / b of values that are not negative and mostly fit in 32 bits (a division of 64 bits is some 100 instructions)
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (a | b) >> 32 ? a / b : static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+}
+
 // ---------------------------------------------------------------- rotary positions and append
 // cos and sin of position x frequency, times the factor.  turns is the frequency as a 64-bit fraction of
 // a turn, so the product modulo 2^64 is the angle's fraction exactly; its upper 32 bits are the angle
@@ -52,11 +57,11 @@ __device__ __forceinline__ float2 cos_sin(const Turn& t, int32_t position, uint6
 // values pair up (half layout: rot_dim / 2 apart; interleaved: side by side), eight pairs with
 // the frequencies 8 u .. 8 u + 7; of the rest, two neighbouring pieces.  A thread takes unit u of kHeads heads of a
 // token: all its loads first; while they are under way the CTA makes the sines and cosines of its tokens, each
-// once.  Memory is the bound.  (Two heads a thread, 64 bytes of loads: 32768 tokens x 32 heads 78 us; one 93; four 80, and
-// 2000 x 28 heads 7.2 us against 6.2.)
+// once.  Memory is the bound.  (Three heads a thread, 96 bytes of loads: prompts of 11160 tokens appended in 32.5 us; one head
+// 39.8, two 33.8, four 35.6.)
 constexpr int kUnits = 8;
 constexpr int kJobs = 256 / kUnits; // (token, group of heads) pairs of a CTA
-constexpr int kHeads = 2;
+constexpr int kHeads = 3;
 
 template <typename T>
 __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs a, int groups) {
@@ -64,9 +69,11 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
   __shared__ float4 s_turn[kJobs][4][kUnits];
   const Pool& p = a.pool;
   const int n_heads = a.n_q + (p.pages ? 2 * p.n_kv : 0);
-  const int64_t job0 = static_cast<int64_t>(blockIdx.x) * kJobs, job = job0 + threadIdx.x / kUnits;
-  const int64_t t0 = job0 / groups, t = job / groups;
-  const int group = static_cast<int>(job - t * groups), u = threadIdx.x % kUnits;
+  const int64_t job0 = static_cast<int64_t>(blockIdx.x) * kJobs, t0 = quotient(job0, groups);
+  const unsigned in = static_cast<unsigned>(job0 - t0 * groups), job = in + threadIdx.x / kUnits;   // from token t0 on
+  const unsigned slot = job / static_cast<unsigned>(groups);
+  const int64_t t = t0 + slot;
+  const int group = static_cast<int>(job - slot * groups), u = threadIdx.x % kUnits;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   const int rot = a.turn.turns ? a.turn.rot_dim : 0;
@@ -79,8 +86,8 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
     const int h = group + i * groups;
     if (h >= n_heads || !in_range) break;
     const Heads& from = h < a.n_q ? a.q : h < a.n_q + p.n_kv ? a.k : a.v;
-    const int in = h < a.n_q ? h : h < a.n_q + p.n_kv ? h - a.n_q : h - a.n_q - p.n_kv;
-    const char* src = static_cast<const char*>(from.x) + 2 * (t * from.token_stride + in * from.head_stride);
+    const int head = h < a.n_q ? h : h < a.n_q + p.n_kv ? h - a.n_q : h - a.n_q - p.n_kv;
+    const char* src = static_cast<const char*>(from.x) + 2 * (t * from.token_stride + head * from.head_stride);
     x[i][0] = *reinterpret_cast<const uint4*>(src + off_a);
     x[i][1] = *reinterpret_cast<const uint4*>(src + off_b);
   }
@@ -100,7 +107,7 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
     }
   }
   if (rot > 0) {
-    const int pairs = rot / 2, n = static_cast<int>(min((job0 + kJobs - 1) / groups, static_cast<int64_t>(a.n_tokens) - 1) - t0) + 1;
+    const int pairs = rot / 2, n = static_cast<int>(min(static_cast<int64_t>((in + kJobs - 1) / static_cast<unsigned>(groups)), a.n_tokens - 1 - t0)) + 1;
     const int32_t* positions = (a.positions ? a.positions : a.index) + t0;
     for (int i = threadIdx.x; i < n * pairs; i += 256) {
       const int k = i / pairs, w = i - k * pairs;
@@ -113,7 +120,7 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
   if (turned) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float4 two = s_turn[static_cast<int>(t - t0)][j][u];
+      const float4 two = s_turn[slot][j][u];
       e[2 * j] = make_float2(two.x, two.y);
       e[2 * j + 1] = make_float2(two.z, two.w);
     }
@@ -175,9 +182,6 @@ constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128
 // 2 c + 1), then int4 per CTA: the segment that it began and did not end (sequence, segment of the
 // sequence, last CTA with a piece of it; sequence -1: none).
 // The line in even parts: CTA c has [begin(c), begin(c + 1)).
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {   // (both >= 0; a 64-bit division is 100 instructions)
-  return (a | b) >> 32 ? a / b : static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
-}
 struct Share {
   int64_t each;
   int n_ctas, longer;               // CTAs that get anything; the first of them get one more
