@@ -220,9 +220,10 @@ cudaError_t launch_pdl(void (*kernel)(Args...), dim3 grid, dim3 block, size_t sm
 // CUtensorMap; rows of `inner` elements, `row_bytes` apart; box box_inner x box_rows.
 cudaError_t make_tensor_map_2d(void* map, const void* base, uint64_t inner, uint64_t rows, uint64_t row_bytes,
                                uint32_t box_inner, uint32_t box_rows);
-// The same with `planes` planes of such rows, plane_bytes apart; a box lies in one plane.
-cudaError_t make_tensor_map_3d(void* map, const void* base, uint64_t inner, uint64_t rows, uint64_t planes,
-                               uint64_t row_bytes, uint64_t plane_bytes, uint32_t box_inner, uint32_t box_rows);
+// 16-bit rows of two halves of half_bytes each, `rows` to a page: (value of a half, half, row, page); a box is
+// box_rows rows of a page; 128-byte swizzle.
+cudaError_t make_tensor_map_halves(void* map, const void* base, uint64_t rows, uint64_t pages, uint32_t half_bytes,
+                                   uint32_t box_rows);
 cudaError_t encode_tensor_maps_u(Plan& plan);
 cudaError_t launch_encode(const Plan& plan, int layer, const void* K, const void* V, int batch,
                           int start, int n_tokens, void* cache, int max_tokens, cudaStream_t st);

@@ -1407,16 +1407,16 @@ cudaError_t make_tensor_map_2d(void* map, const void* base, uint64_t inner, uint
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-cudaError_t make_tensor_map_3d(void* map, const void* base, uint64_t inner, uint64_t rows, uint64_t planes,
-                               uint64_t row_bytes, uint64_t plane_bytes, uint32_t box_inner, uint32_t box_rows) {
+cudaError_t make_tensor_map_halves(void* map, const void* base, uint64_t rows, uint64_t pages, uint32_t half_bytes,
+                                   uint32_t box_rows) {
   auto enc = tensor_map_encoder();
   if (!enc) return cudaErrorNotSupported;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows),
-                              static_cast<cuuint64_t>(planes)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_bytes), static_cast<cuuint64_t>(plane_bytes)};
-  const cuuint32_t box[3] = {box_inner, box_rows, 1};
-  const cuuint32_t es[3] = {1, 1, 1};
-  CUresult r = enc(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+  const cuuint64_t half = half_bytes;
+  const cuuint64_t dims[4] = {half / 2, 2, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(pages)};
+  const cuuint64_t strides[3] = {half, 2 * half, 2 * half * static_cast<cuuint64_t>(rows)};
+  const cuuint32_t box[4] = {half_bytes / 2, 2, box_rows, 1};
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  CUresult r = enc(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
                    const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;

@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
 constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM
-constexpr int kProducers = 2;       // producer warps
+constexpr int kProducers = 4;       // producer warps
 constexpr int kServes = kConsumers / kProducers;
 constexpr int kDecodeThreads = (kConsumers + kProducers) * 32;
 constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less
@@ -293,9 +293,9 @@ struct __align__(16) Unit {
   int b, seg, u, units;
 };
 
-// A warp's piece of a segment that it does not have whole, in shared memory.
+// A warp's piece of a segment that it does not have whole, in shared memory (four heads' rows apart: other banks).
 struct Piece {
-  float sum[kSegHeads][D];
+  float sum[kSegHeads][D + 4];
   float top[kSegHeads], total[kSegHeads];
 };
 struct PieceOf {
@@ -312,7 +312,7 @@ static_assert(sizeof(Piece) <= kStages * kStage && sizeof(Piece) % 16 == 0, "a p
 // What one lane of the producer does for its consumer: the walk over the share's units.
 struct Walk {
   int b, seg, u, len_next;
-  Extent ext;
+  Extent ext;                       // of sequence b
 };
 
 template <typename T>
@@ -323,8 +323,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   extern __shared__ __align__(1024) unsigned char rings[];   // (the copies' permutation goes by 1024-byte blocks)
   __shared__ PieceOf s_of[kW][2];
   __shared__ Unit s_unit[kW][kStages];
-  __shared__ int64_t s_part[kW + kProducers], s_before[kW];
-  __shared__ int s_seq[kW], s_len[kW];
+  __shared__ int64_t s_part[kW + kProducers], s_upto[kT];
+  __shared__ int s_len[kT];
+  __shared__ float s_share[2 * kW][kSegHeads], s_base[kSegHeads], s_prior[kSegHeads], s_total[kSegHeads];
   __shared__ uint64_t s_full[kW][kStages], s_free[kW][kStages];
   __shared__ int s_abort;
   const Pool& p = a.pool;
@@ -347,14 +348,13 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
 
-  // ---- the total, and the sequences in which the warps' shares begin: prefix sums over kT sequences at a time
-  int len = 0;
-  int64_t units = 0, upto = 0;                       // of sequence i0 + tid, with its gaps; up to it within the chunk
+  // ---- the length of the line, and the sequences in which the warps' shares begin: prefix sums over kT sequences
+  // at a time, which every warp looks its own begin up in
+  int64_t in_chunk = 0;
   auto scan = [&](int i0) {
-    const int i = i0 + tid;
-    len = i < a.batch ? __ldg(a.lens + i) : 0;
-    units = i < a.batch ? static_cast<int64_t>(extent_of(a, len).units + kGap) * n_seg : 0;
-    upto = units;
+    const int i = i0 + tid, len = i < a.batch ? __ldg(a.lens + i) : 0;
+    if (blockIdx.x == 0 && (len < 0 || len > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
+    int64_t upto = i < a.batch ? static_cast<int64_t>(extent_of(a, len).units + kGap) * n_seg : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
@@ -362,19 +362,20 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     }
     __syncthreads();                                 // (the last chunk's sums have been read)
     if (lane == 31) s_part[warp] = upto;
+    s_len[tid] = len;
     __syncthreads();
-    int64_t sum = 0;
+    in_chunk = 0;
 #pragma unroll
     for (int w = 0; w < kW + kProducers; ++w) {
-      if (w == warp) upto += sum;
-      sum += s_part[w];
+      if (w == warp) upto += in_chunk;
+      in_chunk += s_part[w];
     }
-    return sum;
+    s_upto[tid] = upto;
   };
   int64_t total = 0;
   for (int i0 = 0; i0 < a.batch; i0 += kT) {
-    total += scan(i0);
-    if (blockIdx.x == 0 && i0 + tid < a.batch && (len < 0 || len > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
+    scan(i0);
+    total += in_chunk;
   }
   Share share;
   share.n_ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kUnitsPerCta - 1) / kUnitsPerCta));
@@ -383,52 +384,47 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   share.each = quotient(total, share.n_ctas);
   share.longer = static_cast<int>(total - share.each * share.n_ctas);
   const int64_t first = share.begin(blockIdx.x), here = share.begin(blockIdx.x + 1) - first;
+  // This warp's consumers: itself, or those that the first lanes of a producer serve.  A lane's walk begins at its
+  // consumer's share: the segment and, behind the gap, the unit there.
+  const int serves = warp < kW ? 1 : kServes, w0 = warp < kW ? warp : (warp - kW) * kServes;
+  const int64_t x_end = first + here * (w0 + min(lane, serves - 1) + 1) / kW;
+  int64_t x = first + here * (w0 + min(lane, serves - 1)) / kW;
+  Walk at;
   {
-    const int64_t begin_last = first + here * (kW - 1) / kW;
     int64_t before = 0;
-    for (int i0 = 0; i0 < a.batch; i0 += kT) {
-      const int64_t sum = a.batch > kT ? scan(i0) : total;
-#pragma unroll
-      for (int w = 0; w < kW; ++w) {
-        const int64_t y = first + here * w / kW - before;
-        if (upto - units <= y && y < upto) {
-          s_seq[w] = i0 + tid;
-          s_len[w] = len;
-          s_before[w] = before + upto - units;
+    for (int i0 = 0;; i0 += kT) {
+      if (a.batch > kT) scan(i0);
+      __syncthreads();
+      for (int k = 0; k < serves; ++k) {
+        const int64_t begin = first + here * (w0 + k) / kW - before;
+        if (begin < 0 || begin >= in_chunk) continue;
+        int c = 0;                                   // the first sequence whose end is past `begin`
+        unsigned past;
+        while (!(past = __ballot_sync(0xffffffffu, s_upto[min(c + lane, kT - 1)] > begin))) c += 32;
+        c += __ffs(past) - 1;
+        if (serves == 1 || lane == k) {
+          at.b = i0 + c;
+          at.ext = extent_of(a, s_len[c]);
+          const int64_t in_seq = begin - (c > 0 ? s_upto[c - 1] : 0);
+          at.seg = static_cast<int>(quotient(in_seq, at.ext.units + kGap));
+          const int in_seg = static_cast<int>(in_seq - static_cast<int64_t>(at.seg) * (at.ext.units + kGap));
+          at.u = max(0, in_seg - kGap);
+          x += max(0, kGap - in_seg);
         }
       }
-      before += sum;
-      if (before > begin_last) break;
+      before += in_chunk;
+      if (before > first + here * (kW - 1) / kW) break;
     }
-    __syncthreads();
   }
-
-  // Where on the line a consumer's share begins: the segment of sequence s_seq and the first unit there, whose place is
-  // moved past the gap.
-  auto begin_of = [&](int w, int64_t& x, Walk& at) {
-    at.b = s_seq[w];
-    at.ext = extent_of(a, s_len[w]);
-    const int64_t in_seq = x - s_before[w];
-    at.seg = static_cast<int>(quotient(in_seq, at.ext.units + kGap));
-    const int in_seg = static_cast<int>(in_seq - static_cast<int64_t>(at.seg) * (at.ext.units + kGap));
-    at.u = max(0, in_seg - kGap);
-    x += max(0, kGap - in_seg);
-  };
-  // second eight tokens and second halves of the heads in a stage
-  const int e_off = p.page_shift > 3 ? 8 * kRow : 16 * kRow, h_off = p.page_shift > 3 ? 16 * kRow : 8 * kRow;
   if (warp >= kW) {
     // ---- a producer: each of its first lanes serves a consumer
-    const bool serves = lane < kServes;
-    const int w = (warp - kW) * kServes + (serves ? lane : 0);
-    int64_t x = first + here * w / kW;
-    const int64_t x_end = serves ? first + here * (w + 1) / kW : 0;
-    Walk at;
-    begin_of(w, x, at);
-    at.len_next = at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
+    const bool on = lane < serves;
+    const int w = w0 + (on ? lane : 0);
+    at.len_next = on && at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
     int id0 = -1, id1 = -1;                          // pages of the unit's halves
     auto fetch_ids = [&]() {
       const int t = (at.ext.lo / kUnit + at.u) * kUnit;
-      if (x >= x_end || t >= at.ext.n) return;
+      if (!on || x >= x_end || t >= at.ext.n) return;
       const int32_t* row = p.table + static_cast<int64_t>(at.b) * p.table_stride;
       id0 = __ldg(row + (t >> p.page_shift));
       id1 = p.page_shift > 3 ? id0 : t + 8 < at.ext.n ? __ldg(row + ((t + 8) >> p.page_shift)) : -1;
@@ -437,7 +433,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     int stage = 0, round = 0;
     uint64_t idle_since = 0;
     for (;;) {
-      const bool work = x < x_end;
+      const bool work = on && x < x_end;
       if (!__any_sync(0xffffffffu, work)) break;
       const bool can = work && (round == 0 || ptx::mbar_test_wait(&s_free[w][stage], (round - 1) & 1));
       if (can) {
@@ -455,20 +451,22 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         unsigned char* to = rings + (w * kStages + stage) * kStage;
         uint64_t* bar = &s_full[w][stage];
         const int row = ((at.seg / seg_blocks) << p.page_shift) + (t & ((1 << p.page_shift) - 1)), v_row = p.n_kv << p.page_shift;
-        // a box is one half of the heads' values: of sixteen tokens where a unit lies in one page, else of eight
-        auto copy = [&](unsigned char* dst, int id) {
-          ptx::tma_load_3d(dst, &map, bar, 0, row, id);
-          ptx::tma_load_3d(dst + h_off, &map, bar, D / 2, row, id);
-          ptx::tma_load_3d(dst + kStage / 2, &map, bar, 0, row + v_row, id);
-          ptx::tma_load_3d(dst + kStage / 2 + h_off, &map, bar, D / 2, row + v_row, id);
-        };
-        if (p.page_shift > 3) {
+        if (p.page_shift > 3) {                      // a unit lies in one page: boxes of sixteen tokens
           ptx::mbar_arrive_expect_tx(bar, ok0 || ok1 ? kStage : 0);
-          if (ok0 || ok1) copy(to, id0);
+          if (ok0 || ok1) {
+            ptx::tma_load_4d(to, &map, bar, 0, 0, row, id0);
+            ptx::tma_load_4d(to + kStage / 2, &map, bar, 0, 0, row + v_row, id0);
+          }
         } else {
           ptx::mbar_arrive_expect_tx(bar, (ok0 ? kStage / 2 : 0) + (ok1 ? kStage / 2 : 0));
-          if (ok0) copy(to, id0);
-          if (ok1) copy(to + e_off, id1);
+          if (ok0) {
+            ptx::tma_load_4d(to, &map, bar, 0, 0, row, id0);
+            ptx::tma_load_4d(to + kStage / 2, &map, bar, 0, 0, row + v_row, id0);
+          }
+          if (ok1) {
+            ptx::tma_load_4d(to + kStage / 4, &map, bar, 0, 0, row, id1);
+            ptx::tma_load_4d(to + kStage / 4 * 3, &map, bar, 0, 0, row + v_row, id1);
+          }
         }
         ++x;
         if (++at.u == at.ext.units) {
@@ -498,18 +496,15 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   } else {
     // ---- a consumer
     const int g = lane / 4, t4 = lane % 4;
-    int64_t x = first + here * warp / kW;
-    const int64_t x_end = first + here * (warp + 1) / kW;
-    Walk at;
-    begin_of(warp, x, at);
     const int64_t x_begin = x;
     unsigned char* ring = rings + warp * (kStages * kStage);
-    // Rows of 128 bytes: [half of the head's values][token] of a page's eight or sixteen tokens, their 16-byte pieces permuted
-    // by the row's number modulo 8.  Keys: matrices (tokens 0 .. 7, 8 .. 15) x (piece, next piece), the A operand of
-    // a score MMA, whose rows are tokens; values: (piece, next) x (tokens 0 .. 7, 8 .. 15), transposed the A
-    // operand of an output MMA, whose rows are dimensions.
-    const uint32_t k_at = (lane / 8 % 2) * e_off + lane % 8 * kRow + ((lane / 16) ^ lane % 8) * 16;
-    const uint32_t v_at = kStage / 2 + (lane / 16) * e_off + lane % 8 * kRow + ((lane / 8 % 2) ^ lane % 8) * 16;
+    // Rows of 128 bytes: [token][half of the head's values], their 16-byte pieces permuted by the row's number modulo
+    // 8.  Keys: matrices (tokens 0 .. 7, 8 .. 15) x (piece, next piece), the A operand of a score MMA,
+    // whose rows are tokens; values: (piece, next) x (tokens 0 .. 7, 8 .. 15), transposed the A operand of an
+    // output MMA, whose rows are dimensions.  (Tokens t and t + 4 of a matrix lie in the same banks.)
+    const int k_row = 2 * (lane / 8 % 2 * 8 + lane % 8), v_row = 2 * (lane / 16 * 8 + lane % 8);
+    const uint32_t k_at = k_row * kRow + ((lane / 16) ^ k_row % 8) * 16;
+    const uint32_t v_at = kStage / 2 + v_row * kRow + ((lane / 8 % 2) ^ v_row % 8) * 16;
     const float unit_scale = a.scale * kLog2e, cap_in = a.cap > 0.0f ? a.scale / a.cap : 0.0f, cap_out = a.cap * kLog2e;
     const bool plain = a.cap <= 0.0f && !a.slopes;
     uint32_t qf[8][2], q_next[8][2];                 // B operand of the score MMAs: column g; of the next segment
@@ -563,10 +558,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       const bool edge = ua.x < ua.y || ua.x + kUnit > ua.z || ua.w != 3;
       if (edge) {                                    // values of masked tokens: their weight is 0, but 0 x NaN is not
         for (int i = lane; i < kUnit * 2 * kRow / 16; i += 32) {
-          const int tok = i / 8 % 16, e = tok / 8;
-          if (!(ua.w >> e & 1) || ua.x + tok < ua.y || ua.x + tok >= ua.z)
-            *reinterpret_cast<uint4*>(ring + stage * kStage + kStage / 2 + e * e_off + i / 128 * h_off + tok % 8 * kRow + i % 8 * 16) =
-                make_uint4(0, 0, 0, 0);
+          const int tok = i / 16;
+          if (!(ua.w >> tok / 8 & 1) || ua.x + tok < ua.y || ua.x + tok >= ua.z)
+            *reinterpret_cast<uint4*>(ring + stage * kStage + kStage / 2 + i * 16) = make_uint4(0, 0, 0, 0);
         }
         ptx::fence_proxy_async_smem();               // (the next copy to the stage comes after)
         __syncwarp();
@@ -576,7 +570,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       for (int j = 0; j < 4; ++j) {
         uint32_t k0[4], k1[4];
         ldsm(k0, base + (k_at ^ 32 * j));
-        ldsm(k1, base + h_off + (k_at ^ 32 * j));
+        ldsm(k1, base + (k_at ^ 32 * j ^ 16) + kRow);
         mma<T>(s, k0, qf[j][0], qf[j][1]);
         mma<T>(s2, k1, qf[4 + j][0], qf[4 + j][1]);
       }
@@ -648,7 +642,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         uint32_t v[4];
-        ldsm_t(v, base + (i / 4) * h_off + (v_at ^ 32 * (i % 4)));
+        ldsm_t(v, base + (i / 4) * kRow + (v_at ^ 32 * (i % 4) ^ (i / 4) * 16));
 #pragma unroll
         for (int y = 0; y < Parts<T>::kN; ++y) mma<T>(acc[i], v, w[0][y], w[1][y]);
       }
@@ -730,54 +724,71 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   if (warp >= kW) return;
   const PieceOf* of = s_of[0];
   const int dim = tid % D;                           // a thread takes this dimension of every second head
-  for (int i = 0; i < 2 * kW; ++i) {
+  unsigned left = __ballot_sync(0xffffffffu, lane < 2 * kW && of[lane % (2 * kW)].b >= 0);
+  while (left) {
+    const int i = __ffs(left) - 1;
     const PieceOf one = of[i];
-    if (one.b < 0) continue;
-    const uint32_t same = __ballot_sync(0xffffffffu, lane < 2 * kW && of[lane % (2 * kW)].b == one.b &&
+    const unsigned same = __ballot_sync(0xffffffffu, lane < 2 * kW && of[lane % (2 * kW)].b == one.b &&
                                                          of[lane % (2 * kW)].seg == one.seg);
-    const int n = 31 - __clz(same);                  // the last piece of the segment
-    const bool begins = i % 2, whole = begins && of[n].ends;
+    left &= ~same;
+    const bool begins = i % 2, whole = begins && of[31 - __clz(same)].ends;
     const int h = one.seg / seg_blocks, head0 = h * a.group + (one.seg % seg_blocks) * kSegHeads;
     const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
+    // each piece's factor, in warp 0: lane (j, q) takes pieces j, j + 4, ... of head q; a warp has one piece at most
+    if (warp == 0) {
+      const int q = lane % kSegHeads;
+      const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
+      float tops[4], best = whole && a.prior_lse && q < n_g ? a.prior_lse[out_row] * kLog2e : -INFINITY, all = 0.0f;
+      const float prior = best;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = lane / kSegHeads + 4 * k;
+        tops[k] = same >> j & 1 ? piece_at(j / 2, j % 2)->top[q] : -INFINITY;
+        best = fmaxf(best, tops[k]);
+      }
+#pragma unroll
+      for (int o = kSegHeads; o < 32; o <<= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
+      const float base = best == -INFINITY ? 0.0f : best;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = lane / kSegHeads + 4 * k;
+        const float f = exp2_of(tops[k] - base);
+        s_share[j][q] = f;
+        if (same >> j & 1) all = fmaf(f, piece_at(j / 2, j % 2)->total[q], all);
+      }
+#pragma unroll
+      for (int o = kSegHeads; o < 32; o <<= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+      const float fp = exp2_of(prior - base);
+      if (lane < n_g) {
+        s_base[q] = best;
+        s_prior[q] = fp;
+        s_total[q] = whole ? all + fp : all;
+        if (whole && a.lse) a.lse[out_row] = base * kLn2 + logf(all + fp);
+      }
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(kW * 32) : "memory");
     float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + begins) * kPiece;
     for (int q = tid / D; q < n_g; q += kW * 32 / D) {
-      const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
-      const float prior = whole && a.prior_lse ? a.prior_lse[out_row] * kLog2e : -INFINITY;
-      const float prior_out = prior > -INFINITY ? a.prior_out[out_row * D + dim] : 0.0f;
-      float tops[2 * kW], top = prior;
+      float sum = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 2 * kW; ++j) {
-        tops[j] = same >> j & 1 ? piece_at(j / 2, j % 2)->top[q] : -INFINITY;
-        top = fmaxf(top, tops[j]);
+      for (int w = 0; w < kW; ++w) {
+        const unsigned mine = same >> 2 * w & 3u;
+        if (mine) sum = fmaf(s_share[2 * w + mine / 2][q], piece_at(w, mine / 2)->sum[q][dim], sum);
       }
-      const float base = top == -INFINITY ? 0.0f : top;
-      float sum = 0.0f, all = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 2 * kW; ++j)
-        if (same >> j & 1) {
-          const float f = exp2_of(tops[j] - base);
-          sum = fmaf(f, piece_at(j / 2, j % 2)->sum[q][dim], sum);
-          all = fmaf(f, piece_at(j / 2, j % 2)->total[q], all);
-        }
       if (whole) {
-        if (prior > -INFINITY) {
-          const float f = exp2_of(prior - base);
-          sum = fmaf(f, prior_out, sum);
-          all += f;
-        }
-        a.out[out_row * D + dim] = all == 0.0f ? 0.0f : sum / all;
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + tid / D), "n"(D) : "memory");   // (the log-sum may replace the prior's)
-        if (a.lse && dim == 0) a.lse[out_row] = base * kLn2 + logf(all);
+        const int64_t out_at = (static_cast<int64_t>(one.b) * a.n_q + head0 + q) * D + dim;
+        if (s_prior[q] > 0.0f) sum = fmaf(s_prior[q], a.prior_out[out_at], sum);
+        a.out[out_at] = s_total[q] == 0.0f ? 0.0f : sum / s_total[q];
       } else {
         piece[q * D + dim] = sum;
         if (dim == 0) {
-          piece[kSegHeads * D + q] = top;
-          piece[kSegHeads * D + kSegHeads + q] = all;
+          piece[kSegHeads * D + q] = s_base[q];
+          piece[kSegHeads * D + kSegHeads + q] = s_total[q];
         }
       }
     }
     if (begins && !whole && tid == 0) desc[blockIdx.x] = make_int4(one.b, one.seg, share.cta_of(one.last_unit), 0);
-    i = n;
+    if (left) asm volatile("bar.sync 1, %0;" ::"n"(kW * 32) : "memory");
   }
 }
 
@@ -937,10 +948,10 @@ size_t decode_workspace(int num_sms) {
 cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
   const int ctas = std::max(1, a.num_sms);
   const auto kernel = dtype == AATC_BF16 ? aatc_paged_decode_kernel<__nv_bfloat16> : aatc_paged_decode_kernel<__half>;
-  CUtensorMap map;                  // [page][token of a head of keys or values][128]
+  CUtensorMap map;                  // [page][token of a head of keys or values][half][64]
   const uint64_t tokens = static_cast<uint64_t>(2) * a.pool.n_kv << a.pool.page_shift;
-  cudaError_t e = make_tensor_map_3d(&map, a.pool.pages, D, tokens, a.pool.n_pages, 2 * kRow, 2 * kRow * tokens, D / 2,
-                                     std::min(kUnit, 1 << a.pool.page_shift));
+  cudaError_t e = make_tensor_map_halves(&map, a.pool.pages, tokens, a.pool.n_pages, kRow,
+                                         std::min(kUnit, 1 << a.pool.page_shift));
   if (e != cudaSuccess) return e;
   e = ensure_smem_optin(reinterpret_cast<const void*>(kernel), kDecodeSmem);
   if (e != cudaSuccess) return e;
