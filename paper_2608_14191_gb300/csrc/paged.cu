@@ -643,8 +643,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       for (int i = 0; i < 8; ++i) {
         uint32_t v[4];
         ldsm_t(v, base + (i / 4) * kRow + (v_at ^ 32 * (i % 4) ^ (i / 4) * 16));
+        // the tensor cores' sums are cut off, not rounded: over a long chain into one accumulator that adds up
+        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int y = 0; y < Parts<T>::kN; ++y) mma<T>(acc[i], v, w[0][y], w[1][y]);
+        for (int y = Parts<T>::kN - 1; y >= 0; --y) mma<T>(part, v, w[0][y], w[1][y]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc[i][y] += part[y];
       }
       __syncwarp();                                  // every lane has read the stage
       if (lane == 0) ptx::mbar_arrive(&s_free[warp][stage]);
