@@ -37,7 +37,8 @@ __device__ __forceinline__ void raise(int32_t* err, int32_t bits) {
   if (err) atomicOr(err, bits);
 }
 
-// a / b of values that are not negative and mostly fit in 32 bits (a division of 64 bits is some 100 instructions)
+// a / b of values that are not negative, of 32 bits or mostly so
+__device__ __forceinline__ int quotient(int a, int b) { return static_cast<unsigned>(a) / static_cast<unsigned>(b); }
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return (a | b) >> 32 ? a / b : static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
 }
@@ -69,7 +70,7 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
   __shared__ float4 s_turn[kJobs][4][kUnits];
   const Pool& p = a.pool;
   const int n_heads = a.n_q + (p.pages ? 2 * p.n_kv : 0);
-  const int64_t job0 = static_cast<int64_t>(blockIdx.x) * kJobs, t0 = quotient(job0, groups);
+  const int64_t job0 = static_cast<int64_t>(blockIdx.x) * kJobs, t0 = quotient(job0, static_cast<int64_t>(groups));
   const unsigned in = static_cast<unsigned>(job0 - t0 * groups), job = in + threadIdx.x / kUnits;   // from token t0 on
   const unsigned slot = job / static_cast<unsigned>(groups);
   const int64_t t = t0 + slot;
@@ -173,7 +174,7 @@ constexpr int kServes = kConsumers / kProducers;
 constexpr int kDecodeThreads = (kConsumers + kProducers) * 32;
 constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less
 constexpr int kStages = 2;          // units of a consumer on their way: keys and values, 8 KB each
-constexpr int kGap = 3;             // units' time that a segment costs beside its units
+constexpr int kGap = 8;             // units' time that a segment costs beside its units
 constexpr int kRow = 128;           // bytes of half a token's key or value: a row in shared memory
 constexpr int kStage = kUnit * 4 * kRow;      // keys, then values
 constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128], maxima [8], totals [8]
@@ -181,13 +182,16 @@ constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128
 // Workspace: pieces [2 n_ctas] (CTA c's share begins inside a segment: piece 2 c; ends inside one that it began:
 // 2 c + 1), then int4 per CTA: the segment that it began and did not end (sequence, segment of the
 // sequence, last CTA with a piece of it; sequence -1: none).
-// The line in even parts: CTA c has [begin(c), begin(c + 1)).
+// The line in even parts: CTA c has [begin(c), begin(c + 1)).  Pos is 32 bits where the table's width bounds the
+// line below 2^31, else 64: divisions of 64 bits are 100 instructions each, in the part of the kernel before its
+// first load.
+template <typename Pos>
 struct Share {
-  int64_t each;
+  Pos each;
   int n_ctas, longer;               // CTAs that get anything; the first of them get one more
-  __device__ int64_t begin(int c) const { return c * each + min(c, longer); }
-  __device__ int cta_of(int64_t at) const {
-    const int64_t big = longer * (each + 1);
+  __device__ Pos begin(int c) const { return c * each + min(c, longer); }
+  __device__ int cta_of(Pos at) const {
+    const Pos big = longer * (each + 1);
     return static_cast<int>(at < big ? quotient(at, each + 1) : longer + quotient(at - big, each));
   }
 };
@@ -298,10 +302,11 @@ struct Piece {
   float sum[kSegHeads][D + 4];
   float top[kSegHeads], total[kSegHeads];
 };
+template <typename Pos>
 struct PieceOf {
   int b, seg;                       // b < 0: none
   int ends;
-  int64_t last_unit;                // of the segment, on the line
+  Pos last_unit;                    // of the segment, on the line
 };
 
 // Shared memory: every consumer's ring of stages, which its piece of the segment that it began takes over at the
@@ -315,15 +320,15 @@ struct Walk {
   Extent ext;                       // of sequence b
 };
 
-template <typename T>
+template <typename T, typename Pos>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
     aatc_paged_decode_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap map) {
   constexpr int kW = kConsumers, kT = kDecodeThreads;
   constexpr float kUnshift = 1.0f / (1 << static_cast<int>(Parts<T>::kShift));
   extern __shared__ __align__(1024) unsigned char rings[];   // (the copies' permutation goes by 1024-byte blocks)
-  __shared__ PieceOf s_of[kW][2];
+  __shared__ PieceOf<Pos> s_of[kW][2];
   __shared__ Unit s_unit[kW][kStages];
-  __shared__ int64_t s_part[kW + kProducers], s_upto[kT];
+  __shared__ Pos s_part[kW + kProducers], s_upto[kT];
   __shared__ int s_len[kT];
   __shared__ float s_share[2 * kW][kSegHeads], s_base[kSegHeads], s_prior[kSegHeads], s_total[kSegHeads];
   __shared__ uint64_t s_full[kW][kStages], s_free[kW][kStages];
@@ -350,14 +355,14 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 
   // ---- the length of the line, and the sequences in which the warps' shares begin: prefix sums over kT sequences
   // at a time, which every warp looks its own begin up in
-  int64_t in_chunk = 0;
+  Pos in_chunk = 0;
   auto scan = [&](int i0) {
     const int i = i0 + tid, len = i < a.batch ? __ldg(a.lens + i) : 0;
     if (blockIdx.x == 0 && (len < 0 || len > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
-    int64_t upto = i < a.batch ? static_cast<int64_t>(extent_of(a, len).units + kGap) * n_seg : 0;
+    Pos upto = i < a.batch ? static_cast<Pos>(extent_of(a, len).units + kGap) * n_seg : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      const Pos y = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += y;
     }
     __syncthreads();                                 // (the last chunk's sums have been read)
@@ -372,54 +377,56 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     }
     s_upto[tid] = upto;
   };
-  int64_t total = 0;
+  Pos total = 0;
   for (int i0 = 0; i0 < a.batch; i0 += kT) {
     scan(i0);
     total += in_chunk;
   }
-  Share share;
-  share.n_ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kUnitsPerCta - 1) / kUnitsPerCta));
+  Share<Pos> share;
+  share.n_ctas = static_cast<int>(min(static_cast<Pos>(gridDim.x), (total + kUnitsPerCta - 1) / kUnitsPerCta));
   if (tid == 0) desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
   if (blockIdx.x >= share.n_ctas) return;
-  share.each = quotient(total, share.n_ctas);
+  share.each = static_cast<Pos>(quotient(total, static_cast<Pos>(share.n_ctas)));
   share.longer = static_cast<int>(total - share.each * share.n_ctas);
-  const int64_t first = share.begin(blockIdx.x), here = share.begin(blockIdx.x + 1) - first;
+  const Pos first = share.begin(blockIdx.x), here = share.begin(blockIdx.x + 1) - first;
   // This warp's consumers: itself, or those that the first lanes of a producer serve.  A lane's walk begins at its
   // consumer's share: the segment and, behind the gap, the unit there.
-  const int serves = warp < kW ? 1 : kServes, w0 = warp < kW ? warp : (warp - kW) * kServes;
-  const int64_t x_end = first + here * (w0 + min(lane, serves - 1) + 1) / kW;
-  int64_t x = first + here * (w0 + min(lane, serves - 1)) / kW;
+  const int w0 = warp < kW ? warp : (warp - kW) * kServes + min(lane, kServes - 1);
+  auto share_of = [&](int w) { return first + static_cast<Pos>(static_cast<int64_t>(here) * w / kW); };
+  const Pos x_end = share_of(w0 + 1);
+  Pos x = share_of(w0);
   Walk at;
   {
-    int64_t before = 0;
+    int skip = 0;
+    Pos before = 0;
     for (int i0 = 0;; i0 += kT) {
       if (a.batch > kT) scan(i0);
       __syncthreads();
-      for (int k = 0; k < serves; ++k) {
-        const int64_t begin = first + here * (w0 + k) / kW - before;
-        if (begin < 0 || begin >= in_chunk) continue;
-        int c = 0;                                   // the first sequence whose end is past `begin`
-        unsigned past;
-        while (!(past = __ballot_sync(0xffffffffu, s_upto[min(c + lane, kT - 1)] > begin))) c += 32;
-        c += __ffs(past) - 1;
-        if (serves == 1 || lane == k) {
-          at.b = i0 + c;
-          at.ext = extent_of(a, s_len[c]);
-          const int64_t in_seq = begin - (c > 0 ? s_upto[c - 1] : 0);
-          at.seg = static_cast<int>(quotient(in_seq, at.ext.units + kGap));
-          const int in_seg = static_cast<int>(in_seq - static_cast<int64_t>(at.seg) * (at.ext.units + kGap));
-          at.u = max(0, in_seg - kGap);
-          x += max(0, kGap - in_seg);
+      const Pos begin = x - before;
+      if (begin >= 0 && begin < in_chunk) {
+        int lo = 0, hi = min(a.batch - i0, kT) - 1;  // the first sequence whose end is past `begin`
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          if (s_upto[mid] > begin) hi = mid;
+          else lo = mid + 1;
         }
+        at.b = i0 + lo;
+        at.ext = extent_of(a, s_len[lo]);
+        const Pos in_seq = begin - (lo > 0 ? s_upto[lo - 1] : 0);
+        at.seg = static_cast<int>(quotient(in_seq, static_cast<Pos>(at.ext.units + kGap)));
+        const int in_seg = static_cast<int>(in_seq - static_cast<Pos>(at.seg) * (at.ext.units + kGap));
+        at.u = max(0, in_seg - kGap);
+        skip = max(0, kGap - in_seg);
       }
       before += in_chunk;
-      if (before > first + here * (kW - 1) / kW) break;
+      if (before > share_of(kW - 1)) break;
     }
+    x += skip;
   }
   if (warp >= kW) {
     // ---- a producer: each of its first lanes serves a consumer
-    const bool on = lane < serves;
-    const int w = w0 + (on ? lane : 0);
+    const bool on = lane < kServes;
+    const int w = w0;
     at.len_next = on && at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
     int id0 = -1, id1 = -1;                          // pages of the unit's halves
     auto fetch_ids = [&]() {
@@ -496,7 +503,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   } else {
     // ---- a consumer
     const int g = lane / 4, t4 = lane % 4;
-    const int64_t x_begin = x;
+    const Pos x_begin = x;
     unsigned char* ring = rings + warp * (kStages * kStage);
     // Rows of 128 bytes: [token][half of the head's values], their 16-byte pieces permuted by the row's number modulo
     // 8.  Keys: matrices (tokens 0 .. 7, 8 .. 15) x (piece, next piece), the A operand of a score MMA,
@@ -540,7 +547,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       const int h = ub.y / seg_blocks, head0 = h * a.group + (ub.y % seg_blocks) * kSegHeads;
       const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
       const bool ends = ub.z == ub.w - 1;
-      const int64_t x_next = x + (ends ? 1 + kGap : 1);
+      const Pos x_next = x + (ends ? 1 + kGap : 1);
       if (fresh) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -726,12 +733,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 
   // ---- join the warps' pieces, which are in the order of the units
   if (warp >= kW) return;
-  const PieceOf* of = s_of[0];
+  const PieceOf<Pos>* of = s_of[0];
   const int dim = tid % D;                           // a thread takes this dimension of every second head
   unsigned left = __ballot_sync(0xffffffffu, lane < 2 * kW && of[lane % (2 * kW)].b >= 0);
   while (left) {
     const int i = __ffs(left) - 1;
-    const PieceOf one = of[i];
+    const PieceOf<Pos> one = of[i];
     const unsigned same = __ballot_sync(0xffffffffu, lane < 2 * kW && of[lane % (2 * kW)].b == one.b &&
                                                          of[lane % (2 * kW)].seg == one.seg);
     left &= ~same;
@@ -951,7 +958,12 @@ size_t decode_workspace(int num_sms) {
 
 cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
   const int ctas = std::max(1, a.num_sms);
-  const auto kernel = dtype == AATC_BF16 ? aatc_paged_decode_kernel<__nv_bfloat16> : aatc_paged_decode_kernel<__half>;
+  const int64_t seqs_units = (static_cast<int64_t>(a.pool.max_pages) << a.pool.page_shift) / kUnit + 1 + kGap;
+  const int n_seg = a.pool.n_kv * ((a.group + kSegHeads - 1) / kSegHeads);
+  const bool narrow = seqs_units * n_seg < ((1ll << 31) - (1 << 16)) / a.batch;
+  const bool bf16 = dtype == AATC_BF16;
+  const auto kernel = narrow ? (bf16 ? aatc_paged_decode_kernel<__nv_bfloat16, int> : aatc_paged_decode_kernel<__half, int>)
+                             : (bf16 ? aatc_paged_decode_kernel<__nv_bfloat16, int64_t> : aatc_paged_decode_kernel<__half, int64_t>);
   CUtensorMap map;                  // [page][token of a head of keys or values][half][64]
   const uint64_t tokens = static_cast<uint64_t>(2) * a.pool.n_kv << a.pool.page_shift;
   cudaError_t e = make_tensor_map_halves(&map, a.pool.pages, tokens, a.pool.n_pages, kRow,

@@ -519,3 +519,32 @@ def test_packed_log_sum(aatc, batch, n_ctx, n_full):
         ref, _ = attend(q[b], torch.cat([keys[b], pool.k[b].double()]), torch.cat([values[b], pool.v[b].double()]))
         assert (joined[b] - ref).abs().max() <= 1e-4 * max(1.0, float(values[b].abs().max()), 6.0)
     assert plan.device_error() == 0
+
+
+@pytest.mark.parametrize("batch,max_pages", [(2, 8388607), (1000, 20), (1000, 20000), (385, 4)])
+def test_decode_wide_tables(batch, max_pages):
+    """More sequences than a CTA has threads, and tables whose width takes the places of tokens past 31 bits."""
+    rng = np.random.default_rng([batch, max_pages])
+    lens = rng.integers(0, 60, batch)
+    lens[-1] = 700
+    per = -(-lens // 256)
+    pages = paged.Pages(1, int(per.sum()), 8, 256, torch.bfloat16, DEV)
+    ids = rng.permutation(int(per.sum()))
+    first = np.concatenate([[0], np.cumsum(per)])
+    table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=DEV)
+    host = np.full((batch, 3), -1)
+    for b in range(batch):
+        host[b, :per[b]] = ids[first[b]:first[b + 1]]
+    table[:, :3] = torch.from_numpy(host).to(DEV, torch.int32)
+    rows = torch.from_numpy(np.repeat(np.arange(batch), lens)).to(DEV, torch.int32)
+    index = torch.from_numpy(np.concatenate([np.arange(n) for n in lens])).to(DEV, torch.int32)
+    k, v = (normal(rng, (int(lens.sum()), 8, 128), torch.bfloat16) for _ in range(2))
+    paged.append(pages, 0, k, v, table, index, rows=rows)
+    q = normal(rng, (batch, 8, 128), torch.bfloat16)
+    out = paged.decode_attention(pages, 0, q, table, torch.from_numpy(lens).to(DEV, torch.int32))
+    start = np.concatenate([[0], np.cumsum(lens)])
+    for b in list(range(0, batch, max(1, batch // 50))) + [batch - 1]:
+        part = slice(int(start[b]), int(start[b + 1]))
+        ref, _ = attend(q[b], k[part], v[part])
+        assert (out[b] - ref).abs().max() <= 2 * SCORE * 6, b
+    assert torch.isfinite(out).all() and pages.device_error() == 0
