@@ -804,8 +804,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 }
 
 // Joins the pieces of the segment that CTA blockIdx.x of the first launch began and did not end; one CTA
-// a query head.  A warp takes every eighth piece, a lane four dimensions, four pieces' loads at a time.
-constexpr int kJoinWarps = 8;
+// a query head.  A warp takes every fourth piece, a lane four dimensions, eight pieces' loads at a time.
+constexpr int kJoinWarps = 4;
 __global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const DecodeArgs a, int n_ctas) {
   __shared__ float so[kJoinWarps][D];
   __shared__ float sm[kJoinWarps], sl[kJoinWarps];
@@ -822,7 +822,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const 
   const float prior_out = a.prior_lse && tid < D ? a.prior_out[out_row * D + tid] : 0.0f;
   float top = -INFINITY, total = 0.0f;
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  constexpr int kAtOnce = 4;
+  constexpr int kAtOnce = 8;
   for (int i0 = warp; i0 < n; i0 += kJoinWarps * kAtOnce) {
     float m[kAtOnce], l[kAtOnce];
     float4 o[kAtOnce];
