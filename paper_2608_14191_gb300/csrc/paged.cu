@@ -58,14 +58,16 @@ __device__ __forceinline__ float2 cos_sin(const Turn& t, int32_t position, uint6
 // values pair up (half layout: rot_dim / 2 apart; interleaved: side by side), eight pairs with
 // the frequencies 8 u .. 8 u + 7; of the rest, two neighbouring pieces.  A thread takes unit u of kHeads heads of a
 // token: all its loads first; while they are under way the CTA makes the sines and cosines of its tokens, each
-// once.  Memory is the bound.  (Three heads a thread, 96 bytes of loads: prompts of 11160 tokens appended in 32.5 us; one head
-// 39.8, two 33.8, four 35.6.)
+// once.  Memory is the bound.  (Prompts of 11160 tokens appended, 36 heads and page writes: three heads a thread, 96
+// bytes of loads, in CTAs of 128 threads 32.0 us; two 32.8; four 33.9; three in CTAs of 256 threads 32.7,
+// where more wait at the barrier.)
 constexpr int kUnits = 8;
-constexpr int kJobs = 256 / kUnits; // (token, group of heads) pairs of a CTA
+constexpr int kAppendThreads = 128;
+constexpr int kJobs = kAppendThreads / kUnits;   // (token, group of heads) pairs of a CTA
 constexpr int kHeads = 3;
 
 template <typename T>
-__global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs a, int groups) {
+__global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const AppendArgs a, int groups) {
   // (cos, sin) of pairs 8 u + 2 j, 8 u + 2 j + 1 of a token at [j][u]: neighbouring units read neighbouring 16 bytes
   __shared__ float4 s_turn[kJobs][4][kUnits];
   const Pool& p = a.pool;
@@ -110,7 +112,7 @@ __global__ void __launch_bounds__(256) aatc_paged_append_kernel(const AppendArgs
   if (rot > 0) {
     const int pairs = rot / 2, n = static_cast<int>(min(static_cast<int64_t>((in + kJobs - 1) / static_cast<unsigned>(groups)), a.n_tokens - 1 - t0)) + 1;
     const int32_t* positions = (a.positions ? a.positions : a.index) + t0;
-    for (int i = threadIdx.x; i < n * pairs; i += 256) {
+    for (int i = threadIdx.x; i < n * pairs; i += kAppendThreads) {
       const int k = i / pairs, w = i - k * pairs;
       reinterpret_cast<float2*>(&s_turn[k][w / 2 % 4][w / 8])[w % 2] = cos_sin(a.turn, __ldg(positions + k), __ldg(a.turn.turns + w));
     }
@@ -949,7 +951,7 @@ cudaError_t launch_append(int dtype, const AppendArgs& a, cudaStream_t st) {
   const int64_t blocks = (static_cast<int64_t>(a.n_tokens) * groups + kJobs - 1) / kJobs;
   if (blocks > INT32_MAX) return cudaErrorNotSupported;
   const auto kernel = dtype == AATC_BF16 ? aatc_paged_append_kernel<__nv_bfloat16> : aatc_paged_append_kernel<__half>;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, a, groups);
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kAppendThreads), 0, st, a, groups);
 }
 
 size_t decode_workspace(int num_sms) {

@@ -14,7 +14,8 @@
 namespace {
 
 PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr;
-PyObject *g_int32, *g_float32, *g_raw_stream, *g_device;      // torch.int32, torch.float32, and the current stream's handle
+PyObject *g_int32, *g_float32, *g_bf16, *g_f16;               // torch's dtypes
+PyObject *g_raw_stream, *g_device;                            // the current stream's handle
 
 struct View {
   int ndim;
@@ -147,20 +148,25 @@ PyObject* answer(F call) {
   return PyLong_FromLong(st);
 }
 
-// rotate(rope address, dtype code, dtype, x, positions, out, backward, stream)
+// rotate(rope address, x, positions, out, backward, stream)
 PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void *rope, *positions, *stream;
-  int32_t code;
   View x, o;
   aatc_heads_t xh, oh;
-  if (n != 8 || !address(a[0], &rope) || !int32_of(a[1], &code) || !heads(a[3], a[2], &x, &xh) ||
-      x.size[0] > INT32_MAX || x.size[1] > INT32_MAX || !flat(a[4], g_int32, 1, x.size[0], 0, 0, &positions) || !positions ||
-      !heads(a[5], a[2], &o, &oh) || o.size[0] != x.size[0] || o.size[1] != x.size[1] || !stream_of(a[7], &stream))
+  if (n != 6 || !address(a[0], &rope)) return not_taken();
+  PyObject* dtype = PyObject_GetAttr(a[1], s_dtype);
+  if (!dtype) return not_taken();
+  Py_DECREF(dtype);                                           // (torch keeps its dtypes)
+  if ((dtype != g_bf16 && dtype != g_f16) || !heads(a[1], dtype, &x, &xh) || x.size[0] > INT32_MAX ||
+      x.size[1] > INT32_MAX || !flat(a[2], g_int32, 1, x.size[0], 0, 0, &positions) || !positions ||
+      !heads(a[3], dtype, &o, &oh) || o.size[0] != x.size[0] || o.size[1] != x.size[1] || !stream_of(a[5], &stream))
     return not_taken();
+  const int32_t code = dtype == g_bf16 ? AATC_BF16 : AATC_F16, backward = PyObject_IsTrue(a[4]);
+  if (backward < 0) return not_taken();
   return answer([&] { return aatc_rotate(static_cast<const aatc_rotary_t*>(rope), code, xh.x, xh.token_stride, xh.head_stride,
                                      static_cast<const int32_t*>(positions), static_cast<int32_t>(x.size[0]),
-                                     static_cast<int32_t>(x.size[1]), a[6] == Py_True, const_cast<void*>(oh.x),
-                                     oh.token_stride, oh.head_stride, stream); });
+                                     static_cast<int32_t>(x.size[1]), backward, const_cast<void*>(oh.x), oh.token_stride,
+                                     oh.head_stride, stream); });
 }
 
 // append(descriptor, layer address, flags address, dtype, n_kv_heads, k, v, table, index, rows, positions, rope address, q,
@@ -238,14 +244,33 @@ PyObject* gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                            static_cast<int32_t*>(flags), stream); });
 }
 
-// setup(torch.int32, torch.float32, current raw stream of a device, current device)
+// copy(descriptor, first layer's address, n_layers, bytes of a layer, pairs, stream); pairs: a C-contiguous int32 buffer [n][2]
+PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void *desc, *base, *stream;
+  int32_t layers;
+  if (n != 6 || !address(a[0], &desc) || !address(a[1], &base) || !int32_of(a[2], &layers) || !stream_of(a[5], &stream))
+    return not_taken();
+  const size_t layer_bytes = PyLong_AsSize_t(a[3]);
+  Py_buffer pairs;
+  if (PyErr_Occurred() || PyObject_GetBuffer(a[4], &pairs, PyBUF_C_CONTIGUOUS | PyBUF_FORMAT) < 0) return not_taken();
+  PyObject* got = nullptr;
+  if (pairs.ndim == 2 && pairs.shape[1] == 2 && pairs.itemsize == 4 && pairs.shape[0] <= INT32_MAX && pairs.format &&
+      pairs.format[0] == 'i' && !pairs.format[1])
+    got = answer([&] { return aatc_pages_copy(static_cast<const aatc_pages_t*>(desc), base, layers, layer_bytes,
+                                              static_cast<const int32_t*>(pairs.buf), static_cast<int32_t>(pairs.shape[0]),
+                                              stream); });
+  PyBuffer_Release(&pairs);
+  return got ? got : not_taken();
+}
+
+// setup(torch.int32, torch.float32, torch.bfloat16, torch.float16, current raw stream of a device, current device)
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) {
-    PyErr_SetString(PyExc_TypeError, "setup takes four objects");
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "setup takes six objects");
     return nullptr;
   }
-  PyObject** to[4] = {&g_int32, &g_float32, &g_raw_stream, &g_device};
-  for (int i = 0; i < 4; ++i) Py_XSETREF(*to[i], Py_NewRef(a[i]));
+  PyObject** to[6] = {&g_int32, &g_float32, &g_bf16, &g_f16, &g_raw_stream, &g_device};
+  for (int i = 0; i < 6; ++i) Py_XSETREF(*to[i], Py_NewRef(a[i]));
   Py_RETURN_NONE;
 }
 
@@ -254,6 +279,7 @@ PyMethodDef methods[] = {
     {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(append)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode)), METH_FASTCALL, nullptr},
     {"gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gather)), METH_FASTCALL, nullptr},
+    {"copy", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(copy)), METH_FASTCALL, nullptr},
     {"setup", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(setup)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -21,7 +21,8 @@ from . import HEAD_DIM, _arg_error, _check, _dev_tensor, _on_device, _stream, lo
 load()                  # (the extension is linked to the library)
 from . import _calls  # noqa: E402
 
-_calls.setup(torch.int32, torch.float32, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+_calls.setup(torch.int32, torch.float32, torch.bfloat16, torch.float16, torch._C._cuda_getCurrentRawStream,
+             torch._C._cuda_getDevice)
 _TYPES = {torch.bfloat16: 0, torch.float16: 1}
 _I32T, _F32T = torch.int32, torch.float32
 _SCALINGS = {"plain": (0, ()), "linear": (1, ()), "ntk": (2, ()), "ramp": (3, ("fast", "slow")),
@@ -187,13 +188,12 @@ def rotate(rope: Rotary, x, positions, out=None, backward: bool = False, stream=
     where = "aatc_rotate"
     if not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
-    if not _on_device(x) or x.dtype not in _TYPES:
-        _arg_error(where, "x must be a device tensor of torch.bfloat16 or torch.float16")
-    if out is None:
+    if out is None and isinstance(x, torch.Tensor):
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    st = _calls.rotate(rope._addr, _TYPES[x.dtype], x.dtype, x, positions, out, bool(backward),
-                       None if stream is None else stream.cuda_stream)
+    st = _calls.rotate(rope._addr, x, positions, out, backward, None if stream is None else stream.cuda_stream)
     if st is None:
+        if not _on_device(x) or x.dtype not in _TYPES:
+            _arg_error(where, "x must be a device tensor of torch.bfloat16 or torch.float16")
         a = _heads(x, where, "x", None)
         n, h = x.shape[0], x.shape[1]
         b = _heads(out, where, "out", x.dtype, h, n)
@@ -304,15 +304,18 @@ def copy_pages(pages: Pages, pairs, stream=None):
     host.  No page may be written twice, or be both read and written."""
     where = "aatc_pages_copy"
     _pages(pages, where)
-    p = pairs
-    if not isinstance(p, np.ndarray) or p.dtype != np.int32 or not p.flags.c_contiguous:
+    st = _calls.copy(pages._addr, pages._layers[0], pages.n_layers, pages.layer_bytes, pairs,
+                     None if stream is None else stream.cuda_stream)
+    if st is None:
         p = np.ascontiguousarray(pairs, dtype=np.int32)
-    if p.size == 0:
-        return
-    if p.ndim != 2 or p.shape[1] != 2:
-        _arg_error(where, "pairs must be [n][2]")
-    _check(pages._lib.aatc_pages_copy(pages._addr, pages._layers[0], pages.n_layers, pages.layer_bytes,
-                                      p.__array_interface__["data"][0], p.shape[0], _stream(stream)), where)
+        if p.size == 0:
+            return
+        if p.ndim != 2 or p.shape[1] != 2:
+            _arg_error(where, "pairs must be [n][2]")
+        st = pages._lib.aatc_pages_copy(pages._addr, pages._layers[0], pages.n_layers, pages.layer_bytes, p.ctypes.data,
+                                        p.shape[0], _stream(stream))
+    if st:
+        _check(st, where)
 
 
 def gather(pages: Pages, layer: int, table, first: int, n_tokens: int, lens=None, out=None, stream=None):
