@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
 // warps an SM were held up by issue latency before the memory was.
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
-constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM
+constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM; a power of two, at most 16
 constexpr int kProducers = 4;       // producer warps
 constexpr int kServes = kConsumers / kProducers;
 constexpr int kDecodeThreads = (kConsumers + kProducers) * 32;
@@ -332,7 +332,6 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   __shared__ Unit s_unit[kW][kStages];
   __shared__ Pos s_part[kW + kProducers], s_upto[kT];
   __shared__ int s_len[kT];
-  __shared__ float s_share[2 * kW][kSegHeads], s_base[kSegHeads], s_prior[kSegHeads], s_total[kSegHeads];
   __shared__ uint64_t s_full[kW][kStages], s_free[kW][kStages];
   __shared__ int s_abort;
   const Pool& p = a.pool;
@@ -560,6 +559,11 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
           slope0 = 2 * t4 < n_g ? a.slopes[head0 + 2 * t4] * kLog2e : 0.0f;
           slope1 = 2 * t4 + 1 < n_g ? a.slopes[head0 + 2 * t4 + 1] * kLog2e : 0.0f;
         }
+        if (a.prior_lse && lane / 4 < n_g) {         // to L2, for whoever finishes the segment
+          const int64_t row = static_cast<int64_t>(ub.x) * a.n_q + head0 + lane / 4;
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(a.prior_out + row * D + lane % 4 * 32));
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(a.prior_lse + row));
+        }
         fresh = false;
       }
       if (ends && x_next < x_end) load_q(ub.y + 1 < n_seg ? ub.x : ub.x + 1, ub.y + 1 < n_seg ? ub.y + 1 : 0, q_next);
@@ -668,7 +672,17 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 
       if (ends || x_next >= x_end) {                 // the segment's or the share's last unit
         fresh = true;
-        const bool begins = x - ub.z >= x_begin;
+        const bool begins = x - ub.z >= x_begin, whole = begins && ends;
+        const int64_t row0 = static_cast<int64_t>(ub.x) * a.n_q + head0 + 2 * t4;
+        float prior[2] = {-INFINITY, -INFINITY}, prior_out[2][16];   // (all loads before the stores, which may be to the same place)
+        const bool joins = whole && a.prior_lse;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (joins && 2 * t4 + i < n_g) {
+            prior[i] = a.prior_lse[row0 + i] * kLog2e;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) prior_out[i][j] = a.prior_out[(row0 + i) * D + g + 8 * j];
+          }
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) {
           l0 += __shfl_xor_sync(0xffffffffu, l0, o);
@@ -676,33 +690,25 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         }
         l0 *= kUnshift;
         l1 *= kUnshift;
+        __syncwarp();                                // (the log-sum may replace the prior's)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int q = 2 * t4 + i;
-          const int64_t out_row = static_cast<int64_t>(ub.x) * a.n_q + head0 + q;
           const float m = i ? m1 : m0, l = i ? l1 : l0;
-          if (begins && ends) {
-            const float prior = a.prior_lse && q < n_g ? a.prior_lse[out_row] * kLog2e : -INFINITY;
-            float top = fmaxf(m, prior);
+          if (whole) {
+            float top = fmaxf(m, prior[i]);
             if (top == -INFINITY) top = 0.0f;
-            const float fm = exp2_of(m - top), fp = exp2_of(prior - top);
+            const float fm = exp2_of(m - top), fp = exp2_of(prior[i] - top);
             const float total = fmaf(l, fm, fp), inv = total == 0.0f ? 0.0f : 1.0f / total;
-            __syncwarp();                            // (the log-sum may be written over the prior's)
             if (q < n_g) {
-              float* to = a.out + out_row * D + g;
-              float o[16];
+              float* to = a.out + (row0 + i) * D + g;
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = acc[j / 2][2 * (j % 2) + i] * (fm * kUnshift);
-              if (fp > 0.0f) {                       // (all loads before the stores, which may go to the same place)
-                float from[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) from[j] = a.prior_out[out_row * D + g + 8 * j];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = fmaf(fp, from[j], o[j]);
+              for (int j = 0; j < 16; ++j) {
+                float o = acc[j / 2][2 * (j % 2) + i] * (fm * kUnshift);
+                if (fp > 0.0f) o = fmaf(fp, prior_out[i][j], o);
+                to[8 * j] = o * inv;
               }
-#pragma unroll
-              for (int j = 0; j < 16; ++j) to[8 * j] = o[j] * inv;
-              if (a.lse && g == 0) a.lse[out_row] = top * kLn2 + logf(total);
+              if (a.lse && g == 0) a.lse[row0 + i] = top * kLn2 + logf(total);
             }
           } else {
             Piece* to = piece_at(warp, begins);
@@ -733,11 +739,11 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     return;
   }
 
-  // ---- join the warps' pieces, which are in the order of the units
+  // ---- join the warps' pieces, which are in the order of the units: a warp takes a query head of a segment
   if (warp >= kW) return;
   const PieceOf<Pos>* of = s_of[0];
-  const int dim = tid % D;                           // a thread takes this dimension of every second head
   unsigned left = __ballot_sync(0xffffffffu, lane < 2 * kW && of[lane % (2 * kW)].b >= 0);
+  int heads_before = 0;
   while (left) {
     const int i = __ffs(left) - 1;
     const PieceOf<Pos> one = of[i];
@@ -747,61 +753,59 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     const bool begins = i % 2, whole = begins && of[31 - __clz(same)].ends;
     const int h = one.seg / seg_blocks, head0 = h * a.group + (one.seg % seg_blocks) * kSegHeads;
     const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
-    // each piece's factor, in warp 0: lane (j, q) takes pieces j, j + 4, ... of head q; a warp has one piece at most
-    if (warp == 0) {
-      const int q = lane % kSegHeads;
-      const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
-      float tops[4], best = whole && a.prior_lse && q < n_g ? a.prior_lse[out_row] * kLog2e : -INFINITY, all = 0.0f;
-      const float prior = best;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int j = lane / kSegHeads + 4 * k;
-        tops[k] = same >> j & 1 ? piece_at(j / 2, j % 2)->top[q] : -INFINITY;
-        best = fmaxf(best, tops[k]);
-      }
-#pragma unroll
-      for (int o = kSegHeads; o < 32; o <<= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-      const float base = best == -INFINITY ? 0.0f : best;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int j = lane / kSegHeads + 4 * k;
-        const float f = exp2_of(tops[k] - base);
-        s_share[j][q] = f;
-        if (same >> j & 1) all = fmaf(f, piece_at(j / 2, j % 2)->total[q], all);
-      }
-#pragma unroll
-      for (int o = kSegHeads; o < 32; o <<= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-      const float fp = exp2_of(prior - base);
-      if (lane < n_g) {
-        s_base[q] = best;
-        s_prior[q] = fp;
-        s_total[q] = whole ? all + fp : all;
-        if (whole && a.lse) a.lse[out_row] = base * kLn2 + logf(all + fp);
-      }
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(kW * 32) : "memory");
     float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + begins) * kPiece;
-    for (int q = tid / D; q < n_g; q += kW * 32 / D) {
-      float sum = 0.0f;
+    for (int q = (warp - heads_before) & (kW - 1); q < n_g; q += kW) {
+      const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
+      float prior = -INFINITY;
+      float4 prior_out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (whole && a.prior_lse) {
+        prior = a.prior_lse[out_row] * kLog2e;
+        prior_out = *reinterpret_cast<const float4*>(a.prior_out + out_row * D + 4 * lane);
+      }
+      const bool has = same >> lane & 1;             // lane j has piece j's factor
+      const Piece* of_lane = piece_at(lane / 2 % kW, lane % 2);
+      const float top = has ? of_lane->top[q] : -INFINITY;
+      float best = fmaxf(top, prior);
 #pragma unroll
-      for (int w = 0; w < kW; ++w) {
-        const unsigned mine = same >> 2 * w & 3u;
-        if (mine) sum = fmaf(s_share[2 * w + mine / 2][q], piece_at(w, mine / 2)->sum[q][dim], sum);
+      for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
+      const float base = best == -INFINITY ? 0.0f : best, f = exp2_of(top - base);
+      float total = has ? f * of_lane->total[q] : 0.0f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (unsigned rest = same; rest; rest &= rest - 1) {
+        const int j = __ffs(rest) - 1;
+        const float fj = __shfl_sync(0xffffffffu, f, j);
+        const float4 v = *reinterpret_cast<const float4*>(&piece_at(j / 2, j % 2)->sum[q][4 * lane]);
+        sum.x = fmaf(fj, v.x, sum.x);
+        sum.y = fmaf(fj, v.y, sum.y);
+        sum.z = fmaf(fj, v.z, sum.z);
+        sum.w = fmaf(fj, v.w, sum.w);
       }
       if (whole) {
-        const int64_t out_at = (static_cast<int64_t>(one.b) * a.n_q + head0 + q) * D + dim;
-        if (s_prior[q] > 0.0f) sum = fmaf(s_prior[q], a.prior_out[out_at], sum);
-        a.out[out_at] = s_total[q] == 0.0f ? 0.0f : sum / s_total[q];
+        const float fp = exp2_of(prior - base);
+        total += fp;
+        if (fp > 0.0f) {
+          sum.x = fmaf(fp, prior_out.x, sum.x);
+          sum.y = fmaf(fp, prior_out.y, sum.y);
+          sum.z = fmaf(fp, prior_out.z, sum.z);
+          sum.w = fmaf(fp, prior_out.w, sum.w);
+        }
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        *reinterpret_cast<float4*>(a.out + out_row * D + 4 * lane) =
+            make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+        __syncwarp();                                // (the log-sum may replace the prior's)
+        if (a.lse && lane == 0) a.lse[out_row] = base * kLn2 + logf(total);
       } else {
-        piece[q * D + dim] = sum;
-        if (dim == 0) {
-          piece[kSegHeads * D + q] = s_base[q];
-          piece[kSegHeads * D + kSegHeads + q] = s_total[q];
+        *reinterpret_cast<float4*>(piece + q * D + 4 * lane) = sum;
+        if (lane == 0) {
+          piece[kSegHeads * D + q] = best;
+          piece[kSegHeads * D + kSegHeads + q] = total;
         }
       }
     }
+    heads_before += n_g;
     if (begins && !whole && tid == 0) desc[blockIdx.x] = make_int4(one.b, one.seg, share.cta_of(one.last_unit), 0);
-    if (left) asm volatile("bar.sync 1, %0;" ::"n"(kW * 32) : "memory");
   }
 }
 
