@@ -96,13 +96,13 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
   }
   // the token's place: keys of all heads of a page, then values; head h of kind c is block (2 id + c) n_kv + h
   char* place = nullptr;
-  const int32_t index = p.pages && in_range ? __ldg(a.index + t) : -1;
+  const int32_t index = p.pages && in_range ? a.index[t] : -1;
   if (index >= 0 && group + (kHeads - 1) * groups >= a.n_q) {
-    const int64_t row = a.rows ? __ldg(a.rows + t) : t;
+    const int64_t row = a.rows ? a.rows[t] : t;
     if (row < 0 || row >= a.n_rows || (index >> p.page_shift) >= p.max_pages) {
       raise(p.err, kBadRow);
     } else {
-      const int32_t id = __ldg(p.table + row * p.table_stride + (index >> p.page_shift));
+      const int32_t id = p.table[row * p.table_stride + (index >> p.page_shift)];
       if (id < 0 || id >= p.n_pages) raise(p.err, kBadPage);
       else
         place = static_cast<char*>(p.pages) + ((static_cast<int64_t>(id) * 2 * p.n_kv << p.page_shift) +
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
     const int32_t* positions = (a.positions ? a.positions : a.index) + t0;
     for (int i = threadIdx.x; i < n * pairs; i += kAppendThreads) {
       const int k = i / pairs, w = i - k * pairs;
-      reinterpret_cast<float2*>(&s_turn[k][w / 2 % 4][w / 8])[w % 2] = cos_sin(a.turn, __ldg(positions + k), __ldg(a.turn.turns + w));
+      reinterpret_cast<float2*>(&s_turn[k][w / 2 % 4][w / 8])[w % 2] = cos_sin(a.turn, positions[k], a.turn.turns[w]);
     }
     __syncthreads();
   }
@@ -160,14 +160,21 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
 // ---------------------------------------------------------------- decode attention
 // The work of a call is its units of 16 tokens: those of sequence 0's kv-head 0, then kv-head 1, ...,
 // then sequence 1's, a (sequence, kv-head) being a segment.  They are laid out on a line, with a gap before
-// every segment for what its begin and end cost a warp; every CTA takes an equal part of the line
-// and each of its consumer warps an eighth of that, so the shares are alike whatever the lengths.  A segment that lies inside a warp's share is finished by the warp, the
-// pieces of one that lies in several warps are joined in shared memory, and those of one in several CTAs
-// through the workspace by the second launch.  (Query heads beyond eight of a kv-head are further segments over
-// the same tokens.)  One more warp brings the units: a lane of it walks each consumer's share, across
-// the segments, and keeps a ring of units under way by TMA.  So the consumers execute little more than the
-// matrix instructions and the softmax: with the walk in every warp a unit took 530 instructions, and eight
-// warps an SM were held up by issue latency before the memory was.
+// every segment for what its begin and end cost a warp; every CTA takes an equal part of the line and each of its
+// consumer warps an eighth of that, so the shares are alike whatever the lengths (with shares by CTA and
+// a barrier per segment, ragged sequences took twice as long as as many tokens in equal ones).  A segment that
+// lies inside a warp's share is finished by the warp, the pieces of one that lies in several warps are joined
+// in shared memory, and those of one in several CTAs through the workspace by the second launch.  (Query heads
+// beyond eight of a kv-head are further segments over the same tokens.)
+// Producer warps bring the units: a lane walks one consumer's share, across the segments, and keeps a ring of
+// units under way by TMA, so the consumers execute little more than the matrix instructions and the softmax
+// (with the walk in every warp a unit took 530 instructions, and eight warps an SM were held up by issue
+// latency before the memory was).  The tensor work is small (4 G flops per byte of cache, G query heads a kv-head), so
+// mma.sync on register fragments serves it: the queries are its eight columns, tokens or dimensions its sixteen
+// rows.  Between the first copy and the last the memory runs at its full rate; what a call takes beyond that is
+// some 3 us to the first copy (dependent loads of lengths and page ids), 2 us from the last one, and the join.
+// Measured (graph replay; K and V bytes over the whole time): 131072 tokens x 8 kv-heads 85 us, 6.3 TB/s; 16 x
+// 8192 x 4 in f16 47 us, 5.7 TB/s; 61 ragged sequences of 57 000 tokens x 8 with cap and prior 50 us; 1001 tokens 7.6 us.
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
 constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM; a power of two, at most 16
@@ -184,6 +191,7 @@ constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128
 // Workspace: pieces [2 n_ctas] (CTA c's share begins inside a segment: piece 2 c; ends inside one that it began:
 // 2 c + 1), then int4 per CTA: the segment that it began and did not end (sequence, segment of the
 // sequence, last CTA with a piece of it; sequence -1: none).
+
 // The line in even parts: CTA c has [begin(c), begin(c + 1)).  Pos is 32 bits where the table's width bounds the
 // line below 2^31, else 64: divisions of 64 bits are 100 instructions each, in the part of the kernel before its
 // first load.
@@ -358,7 +366,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   // at a time, which every warp looks its own begin up in
   Pos in_chunk = 0;
   auto scan = [&](int i0) {
-    const int i = i0 + tid, len = i < a.batch ? __ldg(a.lens + i) : 0;
+    const int i = i0 + tid, len = i < a.batch ? __ldcg(a.lens + i) : 0;
     if (blockIdx.x == 0 && (len < 0 || len > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
     Pos upto = i < a.batch ? static_cast<Pos>(extent_of(a, len).units + kGap) * n_seg : 0;
 #pragma unroll
@@ -396,11 +404,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   auto share_of = [&](int w) { return first + static_cast<Pos>(static_cast<int64_t>(here) * w / kW); };
   const Pos x_end = share_of(w0 + 1);
   Pos x = share_of(w0);
-  Walk at;
+  Walk at = {};
   {
     int skip = 0;
+    bool found = false;
     Pos before = 0;
-    for (int i0 = 0;; i0 += kT) {
+    for (int i0 = 0; i0 < a.batch; i0 += kT) {
       if (a.batch > kT) scan(i0);
       __syncthreads();
       const Pos begin = x - before;
@@ -418,24 +427,25 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         const int in_seg = static_cast<int>(in_seq - static_cast<Pos>(at.seg) * (at.ext.units + kGap));
         at.u = max(0, in_seg - kGap);
         skip = max(0, kGap - in_seg);
+        found = true;
       }
       before += in_chunk;
       if (before > share_of(kW - 1)) break;
     }
-    x += skip;
+    x = found ? x + skip : x_end;                    // (not found: lengths that changed between two reads of them)
   }
   if (warp >= kW) {
     // ---- a producer: each of its first lanes serves a consumer
     const bool on = lane < kServes;
     const int w = w0;
-    at.len_next = on && at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
+    at.len_next = on && at.b + 1 < a.batch ? __ldcg(a.lens + at.b + 1) : 0;
     int id0 = -1, id1 = -1;                          // pages of the unit's halves
     auto fetch_ids = [&]() {
       const int t = (at.ext.lo / kUnit + at.u) * kUnit;
       if (!on || x >= x_end || t >= at.ext.n) return;
       const int32_t* row = p.table + static_cast<int64_t>(at.b) * p.table_stride;
-      id0 = __ldg(row + (t >> p.page_shift));
-      id1 = p.page_shift > 3 ? id0 : t + 8 < at.ext.n ? __ldg(row + ((t + 8) >> p.page_shift)) : -1;
+      id0 = row[t >> p.page_shift];
+      id1 = p.page_shift > 3 ? id0 : t + 8 < at.ext.n ? row[(t + 8) >> p.page_shift] : -1;
     };
     fetch_ids();
     int stage = 0, round = 0;
@@ -484,7 +494,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
             at.seg = 0;
             ++at.b;
             at.ext = extent_of(a, at.len_next);      // (of nothing past the last sequence)
-            at.len_next = at.b + 1 < a.batch ? __ldg(a.lens + at.b + 1) : 0;
+            if (at.b >= a.batch) x = x_end;
+            at.len_next = at.b + 1 < a.batch ? __ldcg(a.lens + at.b + 1) : 0;
           }
         }
         fetch_ids();
@@ -495,7 +506,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         idle_since = 0;
       }
       if (!__any_sync(0xffffffffu, can)) {           // (a consumer that stopped, stops this too)
-        if (*reinterpret_cast<volatile int*>(&s_abort)) break;
+        if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s_abort))) break;
         const uint64_t now = ptx::globaltimer_ns();
         if (idle_since == 0) idle_since = now;
         if (__any_sync(0xffffffffu, now - idle_since > 2000000000ull)) break;
@@ -519,7 +530,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     auto load_q = [&](int b, int seg, uint32_t (&to)[8][2]) {
       const int h = seg / seg_blocks, head0 = h * a.group + (seg % seg_blocks) * kSegHeads;
       const T* q = static_cast<const T*>(a.q.x) + b * a.q.token_stride + (head0 + g) * a.q.head_stride + 2 * t4;
-      const bool in = g < min(kSegHeads, (h + 1) * a.group - head0);
+      const bool in = b < a.batch && g < min(kSegHeads, (h + 1) * a.group - head0);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         to[j][0] = in ? *reinterpret_cast<const uint32_t*>(q + 16 * j) : 0u;
@@ -536,7 +547,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     uint32_t phase = 0;
     bool fresh = true;                               // the next unit is of another segment
     while (x < x_end) {
-      if (!ptx::mbar_wait_bounded(&s_full[warp][stage], phase, &s_abort)) {
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(&s_full[warp][stage], phase, &s_abort))) {
         if (lane == 0) {                             // a copy did not arrive: tell, and stop the others
           raise(p.err, kTimeout);
           *reinterpret_cast<volatile int*>(&s_abort) = 1;
@@ -919,7 +930,7 @@ __global__ void __launch_bounds__(256) aatc_paged_gather_kernel(const GatherArgs
   const int r = blockIdx.y;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
-  const int n = a.lens ? __ldg(a.lens + r) : INT32_MAX;
+  const int n = a.lens ? a.lens[r] : INT32_MAX;
   const int32_t* row = p.table + static_cast<int64_t>(r) * p.table_stride;
   uint4 x[kCopyVecs];
   uint4* to[kCopyVecs];
@@ -935,7 +946,7 @@ __global__ void __launch_bounds__(256) aatc_paged_gather_kernel(const GatherArgs
             ((static_cast<int64_t>(r) * a.n_tokens + i_tok) * p.n_kv + (key ? h : h - p.n_kv)) * kVecs + c % kVecs;
     x[k] = make_uint4(0, 0, 0, 0);
     if (t >= n) continue;
-    const int32_t id = __ldg(row + (t >> p.page_shift));
+    const int32_t id = row[t >> p.page_shift];
     if (id < 0 || id >= p.n_pages) {
       raise(p.err, kBadPage);
       continue;
