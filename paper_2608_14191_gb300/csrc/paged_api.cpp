@@ -28,7 +28,6 @@ int page_shift(const aatc_pages_t* d) {
 
 size_t page_bytes(const aatc_pages_t* d) { return static_cast<size_t>(2) * d->n_kv_heads * d->page_size * D * 2; }
 
-// Strides of `rows` rows: a head's 128 values must not be torn apart by the next one's.
 bool heads_ok(const aatc_heads_t* h) {
   return h && h->x && aligned16(h->x) && h->token_stride % 8 == 0 && h->head_stride % 8 == 0;
 }
@@ -45,7 +44,7 @@ paged::Turn turn(const aatc_rotary_t* r, bool backward) {
 }
 
 bool table_ok(const int32_t* table, int32_t n_rows, int32_t table_stride, int32_t max_pages) {
-  return table && aligned4(table) && n_rows >= 1 && max_pages >= 1 && table_stride >= max_pages;
+  return table && aligned4(table) && n_rows >= 1 && max_pages >= 1 && table_stride >= 0;
 }
 
 paged::Pool pool(const aatc_pages_t* d, void* pages, const int32_t* table, int32_t table_stride, int32_t max_pages,

@@ -70,8 +70,8 @@ bool view_of(PyObject* t, PyObject* dtype, int ndim, View* v) {
 bool heads(PyObject* t, PyObject* dtype, View* v, aatc_heads_t* h) {
   if (!view_of(t, dtype, 3, v) || v->size[2] != AATC_HEAD_DIM || v->stride[2] != 1) return false;
   h->x = v->ptr;
-  h->token_stride = v->stride[0];
-  h->head_stride = v->stride[1];
+  h->token_stride = v->size[0] > 1 ? v->stride[0] : 0;        // (a stride of one row or head means nothing)
+  h->head_stride = v->size[1] > 1 ? v->stride[1] : 0;
   return true;
 }
 

@@ -146,12 +146,12 @@ class Pages:
 # message for what is wrong, and makes the call through ctypes.
 
 def _heads(t, where: str, name: str, dtype, n_heads=None, n_tokens=None):
-    """Checks a [tokens][heads][128] argument; its pointer and strides."""
+    """Checks a [tokens][heads][128] argument; its pointer and strides (0 where there is one of them)."""
     _dev_tensor(t, where, name, dtype, 3, (n_tokens, n_heads, HEAD_DIM))
     s = t.stride()
     if s[2] != 1:
         _arg_error(where, f"the 128 values of a head of {name} must be contiguous")
-    return _Heads(t.data_ptr(), s[0], s[1])
+    return _Heads(t.data_ptr(), s[0] if t.shape[0] > 1 else 0, s[1] if t.shape[1] > 1 else 0)
 
 
 def _ints(t, where: str, name: str, n: int) -> int:
@@ -177,6 +177,13 @@ def _table(t, where: str, n_rows=None):
     return t.data_ptr(), n, t.stride(0) if n > 1 else m, m
 
 
+def _kept(t, stream):
+    """A tensor made here for a call on `stream`: its memory is not given away before that stream is done with it."""
+    if stream is not None and t.is_cuda:
+        t.record_stream(stream)
+    return t
+
+
 def _pages(pages, where: str):
     if not isinstance(pages, Pages):
         _arg_error(where, "pages must be a Pages")
@@ -189,7 +196,7 @@ def rotate(rope: Rotary, x, positions, out=None, backward: bool = False, stream=
     if not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
     if out is None and isinstance(x, torch.Tensor):
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _kept(torch.empty(x.shape, dtype=x.dtype, device=x.device), stream)
     st = _calls.rotate(rope._addr, x, positions, out, backward, None if stream is None else stream.cuda_stream)
     if st is None:
         if not _on_device(x) or x.dtype not in _TYPES:
@@ -216,7 +223,7 @@ def append(pages: Pages, layer: int, k, v, table, index, rows=None, positions=No
     if rope is not None and not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
     if q is not None and q_out is None and _on_device(q):
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _kept(torch.empty(q.shape, dtype=q.dtype, device=q.device), stream)
     base, ro = pages.layer(layer, where), None if rope is None else rope._addr
     st = _calls.append(pages._addr, base, pages._flags, pages.dtype, pages.n_kv_heads, k, v, table, index, rows, positions, ro,
                        q, q_out, None if stream is None else stream.cuda_stream)
@@ -261,7 +268,7 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
     _pages(pages, where)
     base = pages.layer(layer, where)
     if out is None and _on_device(q):
-        out = torch.empty(q.shape, dtype=_F32T, device=q.device)
+        out = _kept(torch.empty(q.shape, dtype=_F32T, device=q.device), stream)
     if prior is None:
         prior = (None, None)
     elif not isinstance(prior, (tuple, list)) or len(prior) != 2 or prior[0] is None or prior[1] is None:
@@ -288,7 +295,7 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
         if batch == 0:
             return out
         if workspace is None:             # (the library refuses one that is too small)
-            workspace = pages.decode_workspace(n_q)
+            workspace = _kept(pages.decode_workspace(n_q), stream)
         elif not _on_device(workspace) or not workspace.is_contiguous():
             _arg_error(where, "workspace must be a contiguous device tensor")
         st = pages._lib.aatc_paged_decode_attention(pages._addr, base, tp, ts, tm, lp, batch, ctypes.byref(qh), n_q,
@@ -329,8 +336,8 @@ def gather(pages: Pages, layer: int, table, first: int, n_tokens: int, lens=None
         if not _on_device(table) or n_tokens < 0:
             _arg_error(where, "table must be a device tensor, n_tokens not negative")
         shape = (table.shape[0], n_tokens, pages.n_kv_heads, HEAD_DIM)
-        k = torch.empty(shape, dtype=pages.dtype, device=pages.device)
-        v = torch.empty(shape, dtype=pages.dtype, device=pages.device)
+        k = _kept(torch.empty(shape, dtype=pages.dtype, device=pages.device), stream)
+        v = _kept(torch.empty(shape, dtype=pages.dtype, device=pages.device), stream)
     elif isinstance(out, (tuple, list)) and len(out) == 2:
         k, v = out
     else:

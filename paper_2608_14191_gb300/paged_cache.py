@@ -63,11 +63,16 @@ class PagedSequences:
             raise ValueError(f"row {row} has a sequence, or is none")
         return row
 
+    def _staged(self, array):
+        """A snapshot of a host array that a copy to the device may read after this call has returned: pinned memory,
+        which torch keeps until the copy is done.  (Plain memory may be read by the device in place, later.)"""
+        t = torch.from_numpy(np.ascontiguousarray(array, np.int32))
+        return t.pin_memory() if self.pages.device.type == "cuda" else t
+
     def _push(self, table: bool):
-        # (pageable memory: the copy has left it when the call returns)
         if table:
-            self.table.copy_(torch.from_numpy(self._table), non_blocking=True)
-        self.lens.copy_(torch.from_numpy(self._lens), non_blocking=True)
+            self.table.copy_(self._staged(self._table), non_blocking=True)
+        self.lens.copy_(self._staged(self._lens), non_blocking=True)
 
     def _release(self, ids):
         np.subtract.at(self.refs, ids, 1)
@@ -140,7 +145,7 @@ class PagedSequences:
         rows = np.repeat(np.fromiter(counts, np.int32, len(counts)), list(counts.values()))
         index = [np.arange(old, old + counts[row], dtype=np.int32) for row, old, _ in take]
         index = np.concatenate(index) if index else np.zeros(0, np.int32)
-        return (torch.from_numpy(np.ascontiguousarray(x, np.int32)).to(self.pages.device, non_blocking=True) for x in (rows, index))
+        return (self._staged(x).to(self.pages.device, non_blocking=True) for x in (rows, index))
 
     def drop_front(self, row: int, tokens: int):
         """Takes the first `tokens` tokens (whole pages) away from a sequence."""

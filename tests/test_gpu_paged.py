@@ -548,3 +548,65 @@ def test_decode_wide_tables(batch, max_pages):
         ref, _ = attend(q[b], k[part], v[part])
         assert (out[b] - ref).abs().max() <= 2 * SCORE * 6, b
     assert torch.isfinite(out).all() and pages.device_error() == 0
+
+
+@pytest.mark.parametrize("page", [8, 16, 128])
+def test_decode_negative_scale_and_bad_ids_by_page(page):
+    """A negative scale under edges and caps; a page outside the pool drops its tokens whatever the page's size."""
+    rng = np.random.default_rng([51, page])
+    pool = Pool(rng, [150, 9, 0], 2, page, torch.bfloat16, scale=0.7)
+    q = normal(rng, (3, 6, 128), torch.bfloat16)
+    check_decode(pool, q, scale=-0.3)
+    check_decode(pool, q, scale=-0.3, cap=4.0, window=33)
+    table = pool.table.clone()
+    table[0, 1], table[1, 0] = pool.pages.n_pages, -7
+    out = paged.decode_attention(pool.pages, 0, q, table, pool.device_lens)
+    left = [t for t in range(150) if t // page != 1]
+    ref, _ = attend(q[0], pool.k[0][left], pool.v[0][left])
+    assert (out[0] - ref).abs().max() <= 2 * SCORE * 6
+    gone = 9 if page > 8 else 8
+    ref, _ = attend(q[1], pool.k[1][gone:], pool.v[1][gone:])
+    assert (out[1] - ref).abs().max() <= 2 * SCORE * 6 and torch.all(out[2] == 0)
+    assert pool.pages.device_error(clear=True) == 4
+
+
+def test_single_rows_and_broadcasts():
+    """One token or one head of any stride; heads and tables that are broadcast; results of a side stream."""
+    rng = np.random.default_rng(52)
+    rope = paged.Rotary(64, 10000.0, device=DEV)
+    x = normal(rng, (8 * 1000,), torch.bfloat16).as_strided((1, 1, 128), (3, 5, 1))
+    at = torch.tensor([77], dtype=torch.int32, device=DEV)
+    check_turned(paged.rotate(rope, x, at), x, at, rope)
+    pool = Pool(rng, [45], 3, 16, torch.bfloat16)
+    q = normal(rng, (1, 1, 128), torch.bfloat16).expand(5, 6, 128)
+    lens = torch.tensor([45, 0, 16, 31, 1], dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = paged.decode_attention(pool.pages, 0, q, pool.table.expand(5, -1), lens, stream=side)
+    k, v = paged.gather(pool.pages, 0, pool.table.expand(5, -1), 3, 40, stream=side)
+    side.synchronize()
+    for b, n in enumerate(lens.tolist()):
+        ref, _ = attend(q[b], pool.k[0][:n], pool.v[0][:n])
+        assert (out[b] - ref).abs().max() <= 2 * SCORE * 6
+        assert torch.equal(k[b], pool.k[0][3:43]) and torch.equal(v[b], pool.v[0][3:43])
+    one = normal(rng, (4, 1, 128), torch.bfloat16)
+    pool.pages.data.zero_()
+    index = torch.arange(4, dtype=torch.int32, device=DEV)
+    paged.append(pool.pages, 0, one.expand(4, 3, 128), one.expand(4, 3, 128), pool.table, index, rows=torch.zeros_like(index))
+    got = paged.gather(pool.pages, 0, pool.table, 0, 4)
+    assert torch.equal(got[0][0], one.expand(4, 3, 128)) and torch.equal(got[1][0], one.expand(4, 3, 128))
+    assert pool.pages.device_error() == 0
+
+
+def test_gather_of_more_rows_than_a_grid_has():
+    rng = np.random.default_rng(53)
+    pages = paged.Pages(1, 70, 1, 8, torch.float16, DEV)
+    pages.data.copy_(normal(rng, pages.data.shape, torch.float16))
+    table = torch.from_numpy(rng.integers(0, 70, (70001, 1))).to(DEV, torch.int32)
+    lens = torch.from_numpy(rng.integers(0, 9, 70001)).to(DEV, torch.int32)
+    k, v = paged.gather(pages, 0, table, 5, 2, lens=lens)
+    for i, got in enumerate((k, v)):
+        want = pages.data[0, table[:, 0].long(), i, 0, 5:7][:, :, None]
+        want = torch.where((torch.arange(5, 7, device=DEV) < lens[:, None])[:, :, None, None], want, 0)
+        assert torch.equal(got, want)
+    assert pages.device_error() == 0
