@@ -70,6 +70,7 @@ struct DecodeArgs {
   float* lse;
   float* ws;
   int num_sms;
+  bool whole;               // every segment to one CTA: nothing to join (set by the launcher)
 };
 
 struct GatherArgs {

@@ -610,3 +610,26 @@ def test_gather_of_more_rows_than_a_grid_has():
         want = torch.where((torch.arange(5, 7, device=DEV) < lens[:, None])[:, :, None, None], want, 0)
         assert torch.equal(got, want)
     assert pages.device_error() == 0
+
+
+@pytest.mark.parametrize("batch", [1, 3, 100, 384, 385])
+@pytest.mark.parametrize("cap_tokens", [256, 264])
+def test_decode_narrow_tables(batch, cap_tokens):
+    """Tables at the width up to which segments stay whole and one past it, by a window too."""
+    rng = np.random.default_rng([batch, cap_tokens])
+    lens = rng.integers(0, cap_tokens + 1, batch)
+    lens[rng.integers(0, batch)] = cap_tokens
+    pool = Pool(rng, [0] * batch, 2, 8, torch.bfloat16)
+    pages = paged.Pages(1, batch * cap_tokens // 8, 2, 8, torch.bfloat16, DEV)
+    ids = rng.permutation(pages.n_pages).reshape(batch, -1)
+    table = torch.from_numpy(ids).to(DEV, torch.int32)
+    rows = torch.from_numpy(np.repeat(np.arange(batch), lens)).to(DEV, torch.int32)
+    index = torch.from_numpy(np.concatenate([np.arange(n) for n in lens])).to(DEV, torch.int32)
+    k, v = (normal(rng, (int(lens.sum()), 2, 128), torch.bfloat16) for _ in range(2))
+    paged.append(pages, 0, k, v, table, index, rows=rows)
+    start = np.concatenate([[0], np.cumsum(lens)])
+    pool.pages, pool.table, pool.device_lens = pages, table, torch.from_numpy(lens).to(DEV, torch.int32)
+    pool.k, pool.v = ([x[start[b]:start[b + 1]] for b in range(batch)] for x in (k, v))
+    q = normal(rng, (batch, 6, 128), torch.bfloat16)
+    check_decode(pool, q)
+    check_decode(pool, q, window=77, cap=20.0)
