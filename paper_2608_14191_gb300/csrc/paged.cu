@@ -3,6 +3,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "aatc_internal.h"
 #include "paged.h"
@@ -182,6 +183,8 @@ constexpr int kProducers = 4;       // producer warps
 constexpr int kServes = kConsumers / kProducers;
 constexpr int kDecodeThreads = (kConsumers + kProducers) * 32;
 constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less
+constexpr int kSeqs = 4;            // sequences of a thread in the prefix sums, where one is not enough
+constexpr int kChunk = kSeqs * kDecodeThreads;
 constexpr int kStages = 2;          // units of a consumer on their way: keys and values, 8 KB each
 constexpr int kGap = 8;             // units' time that a segment costs beside its units
 // Where no segment can have more units than this (by the table's width or the window), the CTAs' parts of the line are
@@ -338,13 +341,13 @@ struct Walk {
 template <typename T, typename Pos>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
     aatc_paged_decode_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap map) {
-  constexpr int kW = kConsumers, kT = kDecodeThreads;
+  constexpr int kW = kConsumers;
   constexpr float kUnshift = 1.0f / (1 << static_cast<int>(Parts<T>::kShift));
   extern __shared__ __align__(1024) unsigned char rings[];   // (the copies' permutation goes by 1024-byte blocks)
   __shared__ PieceOf<Pos> s_of[kW][2];
   __shared__ Unit s_unit[kW][kStages];
-  __shared__ Pos s_part[kW + kProducers], s_upto[kT];
-  __shared__ int s_len[kT];
+  __shared__ Pos s_part[kW + kProducers], s_upto[kChunk];
+  __shared__ int s_len[kChunk];
   __shared__ uint64_t s_full[kW][kStages], s_free[kW][kStages];
   __shared__ int s_abort;
   const Pool& p = a.pool;
@@ -367,13 +370,25 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
 
-  // ---- the length of the line, and the sequences in which the warps' shares begin: prefix sums over kT sequences
+  // ---- the length of the line, and the sequences in which the warps' shares begin: prefix sums over kChunk sequences
   // at a time, which every warp looks its own begin up in
   Pos in_chunk = 0;
-  auto scan = [&](int i0) {
-    const int i = i0 + tid, len = i < a.batch ? __ldcg(a.lens + i) : 0;
-    if (blockIdx.x == 0 && (len < 0 || len > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
-    Pos upto = i < a.batch ? static_cast<Pos>(extent_of(a, len).units + kGap) * n_seg : 0;
+  auto scan = [&](int i0, auto seqs) {
+    constexpr int kN = decltype(seqs)::value;
+    int len[kN];
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      const int i = i0 + kN * tid + k;
+      len[k] = i < a.batch ? __ldcg(a.lens + i) : 0;
+    }
+    Pos own[kN], upto = 0;                        // up to and with each of the thread's, all of the thread's
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      if (blockIdx.x == 0 && (len[k] < 0 || len[k] > p.max_pages << p.page_shift)) raise(p.err, kBadRow);
+      if (i0 + kN * tid + k < a.batch) upto += static_cast<Pos>(extent_of(a, len[k]).units + kGap) * n_seg;
+      own[k] = upto;
+    }
+    const Pos mine = upto;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const Pos y = __shfl_up_sync(0xffffffffu, upto, o);
@@ -381,7 +396,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     }
     __syncthreads();                                 // (the last chunk's sums have been read)
     if (lane == 31) s_part[warp] = upto;
-    s_len[tid] = len;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) s_len[kN * tid + k] = len[k];
     __syncthreads();
     in_chunk = 0;
 #pragma unroll
@@ -389,12 +405,18 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       if (w == warp) upto += in_chunk;
       in_chunk += s_part[w];
     }
-    s_upto[tid] = upto;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) s_upto[kN * tid + k] = upto - mine + own[k];
   };
   Pos total = 0;
-  for (int i0 = 0; i0 < a.batch; i0 += kT) {
-    scan(i0);
-    total += in_chunk;
+  if (a.batch <= kDecodeThreads) {
+    scan(0, std::integral_constant<int, 1>());
+    total = in_chunk;
+  } else {
+    for (int i0 = 0; i0 < a.batch; i0 += kChunk) {
+      scan(i0, std::integral_constant<int, kSeqs>());
+      total += in_chunk;
+    }
   }
   Share<Pos> share;
   share.n_ctas = static_cast<int>(min(static_cast<Pos>(gridDim.x), (total + kUnitsPerCta - 1) / kUnitsPerCta));
@@ -431,12 +453,12 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     int skip = 0;
     bool found = false;
     Pos before = 0;
-    for (int i0 = 0; i0 < a.batch; i0 += kT) {
-      if (a.batch > kT) scan(i0);
+    for (int i0 = 0; i0 < a.batch; i0 += kChunk) {
+      if (a.batch > kChunk) scan(i0, std::integral_constant<int, kSeqs>());
       __syncthreads();
       const Pos begin = x - before;
       if (begin >= 0 && begin < in_chunk) {
-        int lo = 0, hi = min(a.batch - i0, kT) - 1;  // the first sequence whose end is past `begin`
+        int lo = 0, hi = min(a.batch - i0, kChunk) - 1;  // the first sequence whose end is past `begin`
         while (lo < hi) {
           const int mid = (lo + hi) / 2;
           if (s_upto[mid] > begin) hi = mid;
@@ -1003,7 +1025,7 @@ cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
   const int64_t tokens_most = static_cast<int64_t>(a.pool.max_pages) << a.pool.page_shift;
   const int64_t units_most = (a.window > 0 ? std::min<int64_t>(tokens_most, a.window) : tokens_most) / kUnit + 2;
   DecodeArgs args = a;
-  args.whole = units_most <= kWholeUnits + 2 && a.batch <= kDecodeThreads;
+  args.whole = units_most <= kWholeUnits + 2 && a.batch <= kChunk;
   const bool narrow = seqs_units * n_seg < ((1ll << 31) - (1 << 16)) / a.batch;
   const bool bf16 = dtype == AATC_BF16;
   const auto kernel = narrow ? (bf16 ? aatc_paged_decode_kernel<__nv_bfloat16, int> : aatc_paged_decode_kernel<__half, int>)

@@ -633,3 +633,34 @@ def test_decode_narrow_tables(batch, cap_tokens):
     q = normal(rng, (batch, 6, 128), torch.bfloat16)
     check_decode(pool, q)
     check_decode(pool, q, window=77, cap=20.0)
+
+
+@pytest.mark.parametrize("batch", [1535, 1536, 1537, 4000])
+@pytest.mark.parametrize("cap_tokens", [64, 512])
+def test_decode_more_sequences_than_a_chunk(batch, cap_tokens):
+    """Around the number of sequences whose prefix sums a CTA takes at once, with and without the second launch."""
+    rng = np.random.default_rng([batch, cap_tokens])
+    lens = rng.integers(0, 33, batch)
+    lens[[0, batch // 2, batch - 1]] = cap_tokens
+    per = -(-lens // 16)
+    first = np.concatenate([[0], np.cumsum(per)])
+    ids = rng.permutation(int(per.sum()))
+    host = np.full((batch, cap_tokens // 16), -1)
+    for b in range(batch):
+        host[b, :per[b]] = ids[first[b]:first[b + 1]]
+    pages = paged.Pages(1, int(per.sum()), 1, 16, torch.float16, DEV)
+    table = torch.from_numpy(host).to(DEV, torch.int32)
+    rows = torch.from_numpy(np.repeat(np.arange(batch), lens)).to(DEV, torch.int32)
+    index = torch.from_numpy(np.concatenate([np.arange(n) for n in lens])).to(DEV, torch.int32)
+    k, v = (normal(rng, (int(lens.sum()), 1, 128), torch.float16) for _ in range(2))
+    paged.append(pages, 0, k, v, table, index, rows=rows)
+    q = normal(rng, (batch, 4, 128), torch.float16)
+    lse = torch.empty((batch, 4), device=DEV)
+    out = paged.decode_attention(pages, 0, q, table, torch.from_numpy(lens).to(DEV, torch.int32), lse=lse)
+    start = np.concatenate([[0], np.cumsum(lens)])
+    for b in sorted({0, 1, batch // 2, batch - 2, batch - 1, *range(0, batch, 61), *range(min(batch, 1530), min(batch, 1540))}):
+        part = slice(int(start[b]), int(start[b + 1]))
+        ref, ref_lse = attend(q[b], k[part], v[part])
+        assert (out[b] - ref).abs().max() <= 2 * SCORE * 6, b
+        assert lens[b] == 0 or (lse[b] - ref_lse).abs().max() <= SCORE
+    assert torch.isfinite(out).all() and torch.all(out[lens == 0] == 0) and pages.device_error() == 0
