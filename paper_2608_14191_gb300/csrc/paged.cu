@@ -218,13 +218,13 @@ template <typename T>
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
 template <>
 __device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <>
 __device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -245,7 +245,7 @@ __device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t at) {
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of an 8 x 8 matrix of 16-bit values over the warp
   uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
 __device__ __forceinline__ float exp2_of(float x) {            // (-inf: 0)
@@ -337,6 +337,23 @@ struct Walk {
   int b, seg, u, len_next;
   Extent ext;                       // of sequence b
 };
+
+// Query heads of a segment: head0 .. head0 + n, of kv-head h.
+struct SegHeads {
+  int h, head0, n;
+};
+__device__ __forceinline__ SegHeads heads_of(const DecodeArgs& a, int seg_blocks, int seg) {
+  SegHeads s;
+  int block = 0;
+  s.h = seg;
+  if (seg_blocks > 1) {                              // (a division is slow, and rarely needed)
+    s.h = seg / seg_blocks;
+    block = seg - s.h * seg_blocks;
+  }
+  s.head0 = s.h * a.group + block * kSegHeads;
+  s.n = min(kSegHeads, (s.h + 1) * a.group - s.head0);
+  return s;
+}
 
 template <typename T, typename Pos>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
@@ -512,7 +529,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         *reinterpret_cast<int4*>(&un->b) = make_int4(at.b, at.seg, at.u, at.ext.units);
         unsigned char* to = rings + (w * kStages + stage) * kStage;
         uint64_t* bar = &s_full[w][stage];
-        const int row = ((at.seg / seg_blocks) << p.page_shift) + (t & ((1 << p.page_shift) - 1)), v_row = p.n_kv << p.page_shift;
+        const int row = (heads_of(a, seg_blocks, at.seg).h << p.page_shift) + (t & ((1 << p.page_shift) - 1)), v_row = p.n_kv << p.page_shift;
         if (p.page_shift > 3) {                      // a unit lies in one page: boxes of sixteen tokens
           ptx::mbar_arrive_expect_tx(bar, ok0 || ok1 ? kStage : 0);
           if (ok0 || ok1) {
@@ -572,9 +589,9 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
     const bool plain = a.cap <= 0.0f && !a.slopes;
     uint32_t qf[8][2], q_next[8][2];                 // B operand of the score MMAs: column g; of the next segment
     auto load_q = [&](int b, int seg, uint32_t (&to)[8][2]) {
-      const int h = seg / seg_blocks, head0 = h * a.group + (seg % seg_blocks) * kSegHeads;
-      const T* q = static_cast<const T*>(a.q.x) + b * a.q.token_stride + (head0 + g) * a.q.head_stride + 2 * t4;
-      const bool in = b < a.batch && g < min(kSegHeads, (h + 1) * a.group - head0);
+      const SegHeads sh = heads_of(a, seg_blocks, seg);
+      const T* q = static_cast<const T*>(a.q.x) + b * a.q.token_stride + (sh.head0 + g) * a.q.head_stride + 2 * t4;
+      const bool in = b < a.batch && g < sh.n;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         to[j][0] = in ? *reinterpret_cast<const uint32_t*>(q + 16 * j) : 0u;
@@ -600,8 +617,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       }
       const int4 ua = *reinterpret_cast<const int4*>(&s_unit[warp][stage].t);      // t, lo, n, ok
       const int4 ub = *reinterpret_cast<const int4*>(&s_unit[warp][stage].b);      // b, seg, u, units
-      const int h = ub.y / seg_blocks, head0 = h * a.group + (ub.y % seg_blocks) * kSegHeads;
-      const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
+      const SegHeads sh = heads_of(a, seg_blocks, ub.y);
+      const int head0 = sh.head0, n_g = sh.n;
       const bool ends = ub.z == ub.w - 1;
       const Pos x_next = x + (ends ? 1 + kGap : 1);
       if (fresh) {
@@ -634,13 +651,18 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         __syncwarp();
       }
       float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s2[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      {
+        uint32_t k[2][4][4];                         // (all loads before the products: a warp issues in order)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t k0[4], k1[4];
-        ldsm(k0, base + (k_at ^ 32 * j));
-        ldsm(k1, base + (k_at ^ 32 * j ^ 16) + kRow);
-        mma<T>(s, k0, qf[j][0], qf[j][1]);
-        mma<T>(s2, k1, qf[4 + j][0], qf[4 + j][1]);
+        for (int j = 0; j < 4; ++j) {
+          ldsm(k[0][j], base + (k_at ^ 32 * j));
+          ldsm(k[1][j], base + (k_at ^ 32 * j ^ 16) + kRow);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          mma<T>(s, k[0][j], qf[j][0], qf[j][1]);
+          mma<T>(s2, k[1][j], qf[4 + j][0], qf[4 + j][1]);
+        }
       }
       // ---- scores in units of ln 2 after `c`: s[0], s[1] token g, s[2], s[3] token 8 + g; queries 2 t4, 2 t4 + 1
       float c = unit_scale;
@@ -707,16 +729,22 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         w[0][i] = transposed(w[0][i]);
         w[1][i] = transposed(w[1][i]);
       }
+      // the tensor cores' sums are cut off, not rounded: over a long chain into one accumulator that adds up, so a
+      // unit's are added to it by rounded additions.  Four independent chains at a time.
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        uint32_t v[4];
-        ldsm_t(v, base + (i / 4) * kRow + (v_at ^ 32 * (i % 4) ^ (i / 4) * 16));
-        // the tensor cores' sums are cut off, not rounded: over a long chain into one accumulator that adds up
-        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int i0 = 0; i0 < 8; i0 += 4) {
+        uint32_t v[4][4];
+        float part[4][4] = {};
 #pragma unroll
-        for (int y = Parts<T>::kN - 1; y >= 0; --y) mma<T>(part, v, w[0][y], w[1][y]);
+        for (int i = 0; i < 4; ++i) ldsm_t(v[i], base + (i0 / 4) * kRow + (v_at ^ 32 * i ^ (i0 / 4) * 16));
 #pragma unroll
-        for (int y = 0; y < 4; ++y) acc[i][y] += part[y];
+        for (int y = Parts<T>::kN - 1; y >= 0; --y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mma<T>(part[i], v[i], w[0][y], w[1][y]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) acc[i0 + i][y] += part[i][y];
       }
       __syncwarp();                                  // every lane has read the stage
       if (lane == 0) ptx::mbar_arrive(&s_free[warp][stage]);
@@ -806,8 +834,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
                                                          of[lane % (2 * kW)].seg == one.seg);
     left &= ~same;
     const bool begins = i % 2, whole = begins && of[31 - __clz(same)].ends;
-    const int h = one.seg / seg_blocks, head0 = h * a.group + (one.seg % seg_blocks) * kSegHeads;
-    const int n_g = min(kSegHeads, (h + 1) * a.group - head0);
+    const SegHeads sh = heads_of(a, seg_blocks, one.seg);
+    const int head0 = sh.head0, n_g = sh.n;
     float* piece = a.ws + (static_cast<size_t>(blockIdx.x) * 2 + begins) * kPiece;
     for (int q = (warp - heads_before) & (kW - 1); q < n_g; q += kW) {
       const int64_t out_row = static_cast<int64_t>(one.b) * a.n_q + head0 + q;
@@ -828,14 +856,19 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
       float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      for (unsigned rest = same; rest; rest &= rest - 1) {
-        const int j = __ffs(rest) - 1;
-        const float fj = __shfl_sync(0xffffffffu, f, j);
-        const float4 v = *reinterpret_cast<const float4*>(&piece_at(j / 2, j % 2)->sum[q][4 * lane]);
-        sum.x = fmaf(fj, v.x, sum.x);
-        sum.y = fmaf(fj, v.y, sum.y);
-        sum.z = fmaf(fj, v.z, sum.z);
-        sum.w = fmaf(fj, v.w, sum.w);
+      float4 v[kW];                                  // (a warp has one piece of a segment at most; all loads first)
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        const unsigned mine = same >> 2 * w & 3u;
+        v[w] = mine ? *reinterpret_cast<const float4*>(&piece_at(w, mine / 2)->sum[q][4 * lane]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      }
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        const float fw = __shfl_sync(0xffffffffu, f, 2 * w + (same >> (2 * w + 1) & 1u));
+        sum.x = fmaf(fw, v[w].x, sum.x);
+        sum.y = fmaf(fw, v[w].y, sum.y);
+        sum.z = fmaf(fw, v[w].z, sum.z);
+        sum.w = fmaf(fw, v[w].w, sum.w);
       }
       if (whole) {
         const float fp = exp2_of(prior - base);
