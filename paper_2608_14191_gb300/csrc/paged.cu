@@ -192,6 +192,9 @@ constexpr int kGap = 8;             // units' time that a segment costs beside i
 // with it; one sequence x 8 kv-heads of 100 tokens 6.0 against 7.0, of 250 7.3 against 7.1 (and a launch less for the host, 2
 // us), of 500 9.5 against 7.3.
 constexpr int kWholeUnits = 16;
+// Pieces that a segment can have from which sixteen warps join them, not four: 131072 tokens x 1 kv-head 21.2 us against 23.0;
+// but 4000 tokens x 1 kv-head (at most 35 pieces) 9.2 against 7.6.
+constexpr int kManyPieces = 64;
 constexpr int kRow = 128;           // bytes of half a token's key or value: a row in shared memory
 constexpr int kStage = kUnit * 4 * kRow;      // keys, then values
 constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128], maxima [8], totals [8]
@@ -898,8 +901,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
 }
 
 // Joins the pieces of the segment that CTA blockIdx.x of the first launch began and did not end; one CTA
-// a query head.  A warp takes every fourth piece, a lane four dimensions, eight pieces' loads at a time.
-constexpr int kJoinWarps = 4;
+// a query head.  A warp takes every kJoinWarps-th piece, a lane four dimensions, eight pieces' loads at a time.
+template <int kJoinWarps>
 __global__ void __launch_bounds__(kJoinWarps * 32) aatc_paged_join_kernel(const DecodeArgs a, int n_ctas) {
   __shared__ float so[kJoinWarps][D];
   __shared__ float sm[kJoinWarps], sl[kJoinWarps];
@@ -1072,7 +1075,11 @@ cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   e = launch_pdl(kernel, dim3(ctas), dim3(kDecodeThreads), kDecodeSmem, st, args, map);
   if (e != cudaSuccess || args.whole) return e;
-  return launch_pdl(aatc_paged_join_kernel, dim3(ctas, std::min(a.group, kSegHeads)), dim3(kJoinWarps * 32), 0, st, a, ctas);
+  // the segments of a sequence are equally long, so one has pieces in an n_seg-th of the CTAs in use, and two, at most
+  const int64_t used = std::min<int64_t>(ctas, (units_most + kGap + kUnitsPerCta - 1) * n_seg * a.batch / kUnitsPerCta);
+  const dim3 grid(ctas, std::min(a.group, kSegHeads));
+  if (used / n_seg + 2 > kManyPieces) return launch_pdl(aatc_paged_join_kernel<16>, grid, dim3(16 * 32), 0, st, a, ctas);
+  return launch_pdl(aatc_paged_join_kernel<4>, grid, dim3(4 * 32), 0, st, a, ctas);
 }
 
 template <int N>
