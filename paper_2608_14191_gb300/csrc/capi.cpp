@@ -242,7 +242,7 @@ aatc_status_t aatc_selftest_channel_entries(const uint8_t* bits, int32_t* most) 
   return AATC_OK;
 }
 
-int32_t aatc_version(void) { return 200; }   // 0.2.0: plan files, AATC_ERR_IO, planner widths to 16
+int32_t aatc_version(void) { return 300; }   // 0.3.0: paged cache, log-sum of the packed decode
 
 namespace {
 

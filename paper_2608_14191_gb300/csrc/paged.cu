@@ -59,7 +59,7 @@ __device__ __forceinline__ float2 cos_sin(const Turn& t, int32_t position, uint6
 // values pair up (half layout: rot_dim / 2 apart; interleaved: side by side), eight pairs with
 // the frequencies 8 u .. 8 u + 7; of the rest, two neighbouring pieces.  A thread takes unit u of kHeads heads of a
 // token: all its loads first; while they are under way the CTA makes the sines and cosines of its tokens, each
-// once.  Memory is the bound.  (Prompts of 11160 tokens appended, 36 heads and page writes: three heads a thread, 96
+// once.  Memory is the bound.  (Prompts of 9911 tokens appended, 36 heads and page writes: three heads a thread, 96
 // bytes of loads, in CTAs of 128 threads 32.0 us; two 32.8; four 33.9; three in CTAs of 256 threads 32.7,
 // where more wait at the barrier.)
 constexpr int kUnits = 8;
@@ -174,8 +174,8 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
 // mma.sync on register fragments serves it: the queries are its eight columns, tokens or dimensions its sixteen
 // rows.  Between the first copy and the last the memory runs at its full rate; what a call takes beyond that is
 // some 3 us to the first copy (dependent loads of lengths and page ids), 2 us from the last one, and the join.
-// Measured (graph replay; K and V bytes over the whole time): 131072 tokens x 8 kv-heads 85 us, 6.3 TB/s; 16 x
-// 8192 x 4 in f16 47 us, 5.7 TB/s; 61 ragged sequences of 57 000 tokens x 8 with cap and prior 50 us; 1001 tokens 7.6 us.
+// Measured (graph replay; K and V bytes over the whole time): 131072 tokens x 8 kv-heads 86 us, 6.3 TB/s; 16 x
+// 8192 x 4 in f16 47 us, 5.7 TB/s; 61 ragged sequences of 61 876 tokens x 8 with cap and prior 49 us; 1001 tokens 7.4 us.
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
 constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM; a power of two, at most 16

@@ -6,6 +6,8 @@ copy.  `PagedTailCache` serves a batch of sequences of different lengths from bo
 `coded` tokens of every sequence (one number for the batch, as the packed decode has one context length)
 transform-coded, the rest in pages, and one softmax over both.  It is the counterpart of
 `sink_window.SinkWindowCache` for sequences that do not grow in step.
+
+Everything here runs on the current stream.
 """
 from __future__ import annotations
 
@@ -101,7 +103,7 @@ class PagedSequences:
         self._lens[row], self._used[row] = 0, False
         self._push(False)
 
-    def grow(self, counts: dict, stream=None):
+    def grow(self, counts: dict):
         """Room for counts[row] more tokens of every row, with copies of shared pages that they will write
         into.  Returns (rows, index), device int32: where `append` puts the new tokens, packed by
         row in the order of `counts`."""
@@ -140,7 +142,7 @@ class PagedSequences:
                 self.refs[own] = 1
             self._lens[row] += counts[row]
         if pairs:
-            copy_pages(self.pages, np.array(pairs, np.int32), stream=stream)
+            copy_pages(self.pages, np.array(pairs, np.int32))
         self._push(need > 0)
         rows = np.repeat(np.fromiter(counts, np.int32, len(counts)), list(counts.values()))
         index = [np.arange(old, old + counts[row], dtype=np.int32) for row, old, _ in take]
@@ -157,14 +159,14 @@ class PagedSequences:
         self._lens[row] -= tokens
         self._push(True)
 
-    def compact(self, stream=None) -> int:
+    def compact(self) -> int:
         """Moves pages so that those in use are the first ones; returns how many they are."""
         used = np.flatnonzero(self.refs)
         n = len(used)
         holes, far = np.flatnonzero(self.refs[:n] == 0), used[used >= n]
         if len(far):
             pairs = np.stack([far, holes], 1).astype(np.int32)
-            copy_pages(self.pages, pairs, stream=stream)
+            copy_pages(self.pages, pairs)
             place = np.arange(len(self.refs), dtype=np.int32)
             place[far] = holes
             for row in np.flatnonzero(self._used):
@@ -202,48 +204,49 @@ class PagedTailCache:
         self.out = torch.empty((2, batch, dm.n_q_heads, HEAD_DIM), dtype=torch.float32, device=device)
         self.lse = torch.empty((batch, dm.n_q_heads), dtype=torch.float32, device=device)
         self.workspace = self.pages.decode_workspace(dm.n_q_heads)
+        self.packed_workspace = torch.empty(max(1, plan.workspace_bytes(batch, max_tokens) // 4), device=device)
         self._rows = self._index = self._positions = None
 
     def length(self, row: int) -> int:
         return self.coded + self.seqs.length(row)
 
-    def begin(self, counts, stream=None):
+    def begin(self, counts):
         """counts: the number of new tokens of every sequence (their keys, values and queries follow packed,
         sequence after sequence)."""
         if len(counts) != self.batch:
             raise ValueError(f"{self.batch} counts needed")
         if any(self.length(r) + n > self.max_tokens for r, n in enumerate(counts)):
             raise ValueError("packed cache capacity exceeded")
-        self._rows, self._index = self.seqs.grow({r: int(n) for r, n in enumerate(counts)}, stream=stream)
+        self._rows, self._index = self.seqs.grow({r: int(n) for r, n in enumerate(counts)})
         self._positions = self._index + self.coded
 
-    def append(self, layer: int, k, v, q=None, stream=None):
+    def append(self, layer: int, k, v, q=None):
         """k, v bf16 [tokens][n_kv_heads][128] and q [tokens][n_q_heads][128] of the step's tokens; returns the
         turned queries (q itself without a rope)."""
         turn = self.rope is not None
         got = append(self.pages, layer, k, v, self.seqs.table, self._index, rows=self._rows, positions=self._positions,
-                     rope=self.rope, q=q if turn else None, stream=stream)
+                     rope=self.rope, q=q if turn else None)
         return got if turn else q
 
-    def attend(self, layer: int, q, stream=None):
+    def attend(self, layer: int, q):
         """Attention of one query row per sequence, turned, over all its tokens: q bf16 [batch][n_q_heads][128] ->
         fp32 [batch][n_q_heads][128] (overwritten by the next call)."""
         prior = None
         if self.coded:
             decode_attention_sw(self.plan, layer, q, self.caches[layer], 0, self.coded, self.max_tokens, out=self.out[0],
-                                lse=self.lse, stream=stream)
+                                lse=self.lse, workspace=self.packed_workspace)
             prior = (self.out[0], self.lse)
         return decode_attention(self.pages, layer, q, self.seqs.table, self.seqs.lens, out=self.out[1], prior=prior,
-                                workspace=self.workspace, stream=stream)
+                                workspace=self.workspace)
 
-    def end(self, stream=None) -> int:
+    def end(self) -> int:
         """Codes as many tokens of every sequence as the window allows; returns their number."""
         least = min(self.seqs.length(r) for r in range(self.batch))
         n = self.step * max(0, (least - self.window) // self.step)
         if n:
             for layer, cache in enumerate(self.caches):
-                k, v = gather(self.pages, layer, self.seqs.table, 0, n, stream=stream)
-                encode(self.plan, layer, k, v, cache, self.coded, self.max_tokens, stream=stream)
+                k, v = gather(self.pages, layer, self.seqs.table, 0, n)
+                encode(self.plan, layer, k, v, cache, self.coded, self.max_tokens)
             for row in range(self.batch):
                 self.seqs.drop_front(row, n)
             self.coded += n
