@@ -179,14 +179,16 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
 constexpr int kSegHeads = 8;        // query heads of a segment: the columns of the MMAs
 constexpr int kUnit = 16;           // tokens
 constexpr int kConsumers = 8;       // consumer warps of a CTA, one CTA an SM; a power of two, at most 16
-constexpr int kProducers = 4;       // producer warps
+constexpr int kProducers = 4;       // producer warps (131072 tokens: 87.5 us with two, 86.5 with four)
 constexpr int kServes = kConsumers / kProducers;
 constexpr int kDecodeThreads = (kConsumers + kProducers) * 32;
-constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less
+constexpr int kUnitsPerCta = 8;     // fewer CTAs where they would get less (1001 tokens: 7.6 us; 16: 8.5, 24: 9.1)
 constexpr int kSeqs = 4;            // sequences of a thread in the prefix sums, where one is not enough
 constexpr int kChunk = kSeqs * kDecodeThreads;
-constexpr int kStages = 2;          // units of a consumer on their way: keys and values, 8 KB each
-constexpr int kGap = 8;             // units' time that a segment costs beside its units
+constexpr int kStages = 2;          // units of a consumer on their way: keys and values, 8 KB each (one: 131072 tokens 104 us,
+                                    // 86 with two, as with three when those fitted)
+constexpr int kGap = 8;             // units' time that a segment costs beside its units (61 ragged sequences: 5 49.8 us,
+                                    // 8 49.7, 12 51.3; 600 of up to 40 tokens 24.7, 24.1, 22.4)
 // Where no segment can have more units than this (by the table's width or the window), the CTAs' parts of the line are
 // moved to whole segments and there is no second launch.  300 sequences of 1 to 40 tokens x 4 kv-heads: 10.7 us against 17.1
 // with it; one sequence x 8 kv-heads of 100 tokens 6.0 against 7.0, of 250 7.3 against 7.1 (and a launch less for the host, 2
@@ -205,7 +207,7 @@ constexpr int kPiece = kSegHeads * (D + 2);   // floats of a piece: sums [8][128
 
 // The line in even parts: CTA c has [begin(c), begin(c + 1)).  Pos is 32 bits where the table's width bounds the
 // line below 2^31, else 64: divisions of 64 bits are 100 instructions each, in the part of the kernel before its
-// first load.
+// first load (1001 tokens: 7.6 us with 32 bits, 8.2 with 64).
 template <typename Pos>
 struct Share {
   Pos each;
@@ -1098,7 +1100,8 @@ static cudaError_t launch_copy_n(void* pages, size_t page_bytes, int n_layers, s
 
 cudaError_t launch_copy(void* pages, size_t page_bytes, int n_layers, size_t layer_stride, const int32_t* pairs,
                         int n_pairs, cudaStream_t st) {
-  constexpr int kMost = 500, kFew = 30;                        // pairs of a launch: 4000 bytes of parameters, or 240
+  // pairs of a launch: 4000 bytes of parameters, or 240 (host time of a copy of 7 pairs 2.7 us with these, 3.1 with those)
+  constexpr int kMost = 500, kFew = 30;
   for (int i0 = 0; i0 < n_pairs; i0 += kMost) {
     const int n = std::min(kMost, n_pairs - i0);
     const cudaError_t e = (n <= kFew ? launch_copy_n<kFew> : launch_copy_n<kMost>)(pages, page_bytes, n_layers, layer_stride,
