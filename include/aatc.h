@@ -612,8 +612,8 @@ aatc_status_t aatc_pages_copy(const aatc_pages_t* desc, void* pages, int32_t n_l
  *   k_out, v_out : device [n_rows][n_tokens][n_kv_heads][128], contiguous (what aatc_encode takes)
  *   lens         : device int32 [n_rows] or NULL; tokens at or past their sequence's length are written
  *                  as zeros and their pages are not read
- * Errors: AATC_ERR_INVALID_ARG, AATC_ERR_CAPACITY (first + n_tokens > max_pages * page_size).  n_tokens or n_rows
- * == 0 is a no-op.
+ * Errors: AATC_ERR_INVALID_ARG, AATC_ERR_CAPACITY (first + n_tokens > max_pages * page_size, or past 2^31 - 1).
+ * n_tokens or n_rows == 0 is a no-op.
  */
 aatc_status_t aatc_paged_gather(const aatc_pages_t* desc, const void* pages, const int32_t* table, int32_t n_rows,
                                 int32_t table_stride, int32_t max_pages, int32_t first, int32_t n_tokens,

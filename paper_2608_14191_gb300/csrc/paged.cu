@@ -309,7 +309,7 @@ __device__ __forceinline__ Extent extent_of(const DecodeArgs& a, int len) {
   Extent e;
   e.n = min(max(len, 0), a.pool.max_pages << a.pool.page_shift);
   e.lo = a.window > 0 ? max(0, e.n - a.window) : 0;
-  e.units = max(1, (e.n + kUnit - 1) / kUnit - e.lo / kUnit);
+  e.units = max(1, e.n / kUnit + (e.n % kUnit > 0) - e.lo / kUnit);   // (n + 15 may pass 31 bits)
   return e;
 }
 
@@ -645,7 +645,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
       }
       if (ends && x_next < x_end) load_q(ub.y + 1 < n_seg ? ub.x : ub.x + 1, ub.y + 1 < n_seg ? ub.y + 1 : 0, q_next);
       const uint32_t base = ptx::smem_u32(ring) + stage * kStage;
-      const bool edge = ua.x < ua.y || ua.x + kUnit > ua.z || ua.w != 3;
+      const bool edge = ua.x < ua.y || ua.z - ua.x < kUnit || ua.w != 3;
       if (edge) {                                    // values of masked tokens: their weight is 0, but 0 x NaN is not
         for (int i = lane; i < kUnit * 2 * kRow / 16; i += 32) {
           const int tok = i / 16;

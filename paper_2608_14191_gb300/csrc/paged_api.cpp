@@ -270,7 +270,9 @@ aatc_status_t aatc_paged_gather(const aatc_pages_t* desc, const void* pages, con
   if (!pages || !aligned16(pages) || !table_ok(table, n_rows, table_stride, max_pages) || !aligned4(lens) || !k_out ||
       !v_out || !aligned16(k_out) || !aligned16(v_out) || !aligned4(dev_flags))
     return AATC_ERR_INVALID_ARG;
-  if (static_cast<int64_t>(first) + n_tokens > static_cast<int64_t>(max_pages) * desc->page_size) return AATC_ERR_CAPACITY;
+  if (static_cast<int64_t>(first) + n_tokens >
+      std::min<int64_t>(static_cast<int64_t>(max_pages) * desc->page_size, INT32_MAX))
+    return AATC_ERR_CAPACITY;
   paged::GatherArgs a = {};
   a.pool = pool(desc, const_cast<void*>(pages), table, table_stride, max_pages, dev_flags);
   a.n_rows = n_rows;

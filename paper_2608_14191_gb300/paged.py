@@ -286,6 +286,8 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
         lp = _ints(lens, where, "lens", batch)
         op = _floats(out, where, "out", (batch, n_q, HEAD_DIM))
         ep = None if lse is None else _floats(lse, where, "lse", (batch, n_q))
+        if not 0 <= window < 1 << 31:
+            _arg_error(where, "window must be in 0 .. 2^31 - 1")
         how = _Decode(scale, cap, window)
         if slopes is not None:
             how.slopes = _floats(slopes, where, "slopes", (n_q,))
@@ -346,6 +348,8 @@ def gather(pages: Pages, layer: int, table, first: int, n_tokens: int, lens=None
                        None if stream is None else stream.cuda_stream)
     if st is None:
         tp, tn, ts, tm = _table(table, where)
+        if not (0 <= first < 1 << 31 and 0 <= n_tokens < 1 << 31):
+            _arg_error(where, "first and n_tokens must be in 0 .. 2^31 - 1")
         shape = (tn, int(n_tokens), pages.n_kv_heads, HEAD_DIM)
         for t in (k, v):
             if not _on_device(t) or t.dtype != pages.dtype or t.shape != shape or not t.is_contiguous():

@@ -179,3 +179,20 @@ def test_packed_lse_refusals(aatc, monkeypatch):
     refused(aatc.AatcError, lambda: aatc.decode_attention_sw(plan, 0, q, cache, 0, 5, 9, lse=torch.zeros((1, 8)), stream=S))
     lib = aatc.load()
     assert lib.aatc_decode_attention_lse(None, 0, 16, 16, 1, 0, 1, 1, None, None, 0, 0, 16, None, 16, 1 << 20, None) == 1
+
+
+def test_places_past_31_bits_are_refused(paged, aatc):
+    """Tables wide enough for more than 2^31 - 1 tokens: a gather past that and a decode are refused before anything is read."""
+    lib, d = aatc.load(), paged._Desc(0, 1, 256, 1 << 20)
+    at, wide = ctypes.c_void_p(4096), 1 << 24
+    gather = lambda first, n, pages: lib.aatc_paged_gather(ctypes.byref(d), at, at, 1, pages, pages, first, n, None, at, at, None, None)  # noqa: E731
+    assert gather(2**31 - 1, 1, wide) == 3 and gather(2**31 - 10, 2**31 - 1, wide) == 3
+    assert gather(100, 157, 1) == 3 and gather(100, 0, 1) == 0
+    how, q = paged._Decode(1.0, 0.0, 0), paged._Heads(4096, 128, 128)
+    assert lib.aatc_paged_decode_attention(ctypes.byref(d), at, at, wide, wide, at, 1, ctypes.byref(q), 1, ctypes.byref(how), at, None, at,
+                                           1 << 30, None, None) == 1
+    p, t, n = pool(paged), torch.zeros((3, 4), dtype=i32), torch.ones(3, dtype=i32)
+    for first in (2**31, 2**32 + 1):
+        refused(aatc.AatcError, lambda: paged.gather(p, 0, t, first, 1, stream=S))
+    refused(aatc.AatcError, lambda: paged.decode_attention(p, 0, torch.zeros((3, 2, 128), dtype=bf16), t, n, window=2**32 + 5,
+                                                           workspace=torch.zeros(1 << 20), stream=S))
