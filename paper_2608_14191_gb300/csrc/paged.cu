@@ -60,8 +60,8 @@ __device__ __forceinline__ float2 cos_sin(const Turn& t, int32_t position, uint6
 // the frequencies 8 u .. 8 u + 7; of the rest, two neighbouring pieces.  A thread takes unit u of kHeads heads of a
 // token: all its loads first; while they are under way the CTA makes the sines and cosines of its tokens, each
 // once.  Memory is the bound.  (Prompts of 9911 tokens appended, 36 heads and page writes: three heads a thread, 96
-// bytes of loads, in CTAs of 128 threads 32.0 us; two 32.8; four 33.9; three in CTAs of 256 threads 32.7,
-// where more wait at the barrier.)
+// bytes of loads, in CTAs of 128 threads 29.0 us, 6.3 TB/s read and written; two 30.4; three in CTAs of 256 threads
+// 29.6, where more wait at the barrier; 32.0 where the page's id was waited for before the angles.)
 constexpr int kUnits = 8;
 constexpr int kAppendThreads = 128;
 constexpr int kJobs = kAppendThreads / kUnits;   // (token, group of heads) pairs of a CTA
@@ -95,21 +95,16 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
     x[i][0] = *reinterpret_cast<const uint4*>(src + off_a);
     x[i][1] = *reinterpret_cast<const uint4*>(src + off_b);
   }
-  // the token's place: keys of all heads of a page, then values; head h of kind c is block (2 id + c) n_kv + h
-  char* place = nullptr;
-  const int32_t index = p.pages && in_range ? a.index[t] : -1;
-  if (index >= 0 && group + (kHeads - 1) * groups >= a.n_q) {
-    const int64_t row = a.rows ? a.rows[t] : t;
-    if (row < 0 || row >= a.n_rows || (index >> p.page_shift) >= p.max_pages) {
-      raise(p.err, kBadRow);
-    } else {
-      const int32_t id = p.table[row * p.table_stride + (index >> p.page_shift)];
-      if (id < 0 || id >= p.n_pages) raise(p.err, kBadPage);
-      else
-        place = static_cast<char*>(p.pages) + ((static_cast<int64_t>(id) * 2 * p.n_kv << p.page_shift) +
-                                               (index & ((1 << p.page_shift) - 1))) * (2 * D);
-    }
+  // the token's page, whose id comes while the angles are made
+  const bool stores = p.pages && in_range && group + (kHeads - 1) * groups >= a.n_q;
+  const int32_t index = stores ? a.index[t] : -1;
+  const int64_t row = stores && a.rows ? a.rows[t] : t;
+  bool placed = index >= 0;
+  if (placed && (row < 0 || row >= a.n_rows || (index >> p.page_shift) >= p.max_pages)) {
+    raise(p.err, kBadRow);
+    placed = false;
   }
+  const int32_t id = placed ? p.table[row * p.table_stride + (index >> p.page_shift)] : 0;
   if (rot > 0) {
     const int pairs = rot / 2, n = static_cast<int>(min(static_cast<int64_t>((in + kJobs - 1) / static_cast<unsigned>(groups)), a.n_tokens - 1 - t0)) + 1;
     const int32_t* positions = (a.positions ? a.positions : a.index) + t0;
@@ -120,6 +115,13 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
     __syncthreads();
   }
   if (!in_range) return;
+  if (placed && (id < 0 || id >= p.n_pages)) {
+    raise(p.err, kBadPage);
+    placed = false;
+  }
+  // keys of all heads of a page, then values; head h of kind c is block (2 id + c) n_kv + h
+  char* place = static_cast<char*>(p.pages) +
+                ((static_cast<int64_t>(id) * 2 * p.n_kv << p.page_shift) + (index & ((1 << p.page_shift) - 1))) * (2 * D);
   float2 e[8];
   if (turned) {
 #pragma unroll
@@ -151,7 +153,7 @@ __global__ void __launch_bounds__(kAppendThreads) aatc_paged_append_kernel(const
     }
     char* dst;
     if (h < a.n_q) dst = static_cast<char*>(a.q_out) + 2 * (t * a.q_out_token_stride + h * a.q_out_head_stride);
-    else if (place) dst = place + (static_cast<int64_t>(h - a.n_q) << p.page_shift) * (2 * D);
+    else if (placed) dst = place + (static_cast<int64_t>(h - a.n_q) << p.page_shift) * (2 * D);
     else continue;
     *reinterpret_cast<uint4*>(dst + off_a) = x[i][0];
     *reinterpret_cast<uint4*>(dst + off_b) = x[i][1];
