@@ -272,12 +272,14 @@ __device__ __forceinline__ float tanh_of(float x) {
 // nothing of it: bf16, three truncations of eight significant bits (all of p's 24); f16, a truncation and the
 // rounded rest (22 bits; p <= 2^14 and its scale keep the rest above the format's smallest step for
 // any p over 2^-30 of the largest).  No part is negative, and no bf16 part zero, as an infinite value
-// times it would turn into NaN.
+// times it would turn into NaN.  f16 parts can be zero, so a unit with infinities or NaN among its values is summed
+// by `exact_unit`.
 template <typename T>
 struct Parts;
 template <>
 struct Parts<__nv_bfloat16> {
   static constexpr int kN = 3;
+  static constexpr bool kMayBeZero = false;
   static constexpr float kShift = 0.0f;                        // log2 of the scale on p
   static __device__ __forceinline__ void split(float p, float q, uint32_t (&out)[3]) {
 #pragma unroll
@@ -292,6 +294,7 @@ struct Parts<__nv_bfloat16> {
 template <>
 struct Parts<__half> {
   static constexpr int kN = 2;
+  static constexpr bool kMayBeZero = true;
   static constexpr float kShift = 6.0f;
   static __device__ __forceinline__ void split(float p, float q, uint32_t (&out)[2]) {
     const __half2 h = __halves2half2(__float2half_rz(p), __float2half_rz(q));
@@ -301,6 +304,28 @@ struct Parts<__half> {
     out[1] = *reinterpret_cast<const uint32_t*>(&l);
   }
 };
+
+// The sums of half a unit's values (64 dimensions, a row of kRow bytes a token) under the fp32 weights s themselves: what the
+// MMAs give, but where a value is infinite or NaN also that.  `values`: the first row, in the order in which the copies leave them
+// (`half`: which one of the two); lane (g, t4) has the weights of tokens g (s[0], s[1]) and 8 + g (s[2], s[3]) for queries
+// 2 t4, 2 t4 + 1.
+__device__ __forceinline__ void exact_unit(const unsigned char* values, int half, const float (&s)[4], float (&part)[4][4]) {
+  const int lane = threadIdx.x % 32, g = lane / 4, t4 = lane % 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) part[i][0] = part[i][1] = part[i][2] = part[i][3] = 0.0f;
+#pragma unroll 1
+  for (int tok = 0; tok < kUnit; ++tok) {
+    const int from = tok % 8 * 4 + t4, row = 2 * tok + half;
+    const float w0 = __shfl_sync(0xffffffffu, tok < 8 ? s[0] : s[2], from);
+    const float w1 = __shfl_sync(0xffffffffu, tok < 8 ? s[1] : s[3], from);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {                              // dimensions 8 i + g of the half
+      const float v = __half2float(reinterpret_cast<const __half*>(values + row * kRow + (i ^ row % 8) * 16)[g]);
+      part[i / 2][i % 2 * 2] = fmaf(w0, v, part[i / 2][i % 2 * 2]);
+      part[i / 2][i % 2 * 2 + 1] = fmaf(w1, v, part[i / 2][i % 2 * 2 + 1]);
+    }
+  }
+}
 
 // First token and unit count of a sequence: the tokens [lo, n) in units from lo / 16 on; one unit, of nothing,
 // for an empty one (somebody has to write its result).
@@ -748,6 +773,15 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
         for (int y = Parts<T>::kN - 1; y >= 0; --y)
 #pragma unroll
           for (int i = 0; i < 4; ++i) mma<T>(part[i], v[i], w[0][y], w[1][y]);
+        if constexpr (Parts<T>::kMayBeZero) {
+          float probe[4] = {};                       // not finite where a sum is not
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) probe[y] += part[i][y];
+          if (__any_sync(0xffffffffu, !(fabsf((probe[0] + probe[1]) + (probe[2] + probe[3])) < INFINITY)))
+            exact_unit(ring + stage * kStage + kStage / 2, i0 / 4, s, part);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll

@@ -1,0 +1,60 @@
+"""The paged operators where types, streams and arguments end, on the GPU against their definitions in 64 bits.  Tolerances as
+in test_gpu_paged; the ones that are finer are derived at their test."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_14191_gb300 import paged
+from test_gpu_paged import DEV, DTYPES, SCORE, Pool, attend, normal
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _built(aatc):
+    return aatc
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("page", [8, 16, 64])
+def test_decode_infinite_values(page, dtype):
+    """Live infinities and NaN among the values come out as the formula has them, whatever the weight: of a token alone, of
+    equal weights, of weights 2^-25 and 2^-40 of the largest, in the first unit and in the last one."""
+    rng = np.random.default_rng([61, page])
+    pool = Pool(rng, [1, 40, 90, 50, 1500, 17], 2, page, dtype)
+    q = normal(rng, (6, 6, 128), dtype)
+    inf, nan = math.inf, math.nan
+
+    def put(r, t, kind, head, dims, values):
+        to = (pool.k, pool.v)[kind][r]
+        to[t, head, dims] = torch.tensor(values, dtype=dtype, device=DEV)
+        pool.write(r, t, pool.k[r][t:t + 1], pool.v[r][t:t + 1])
+
+    put(0, 0, 1, 0, [9, 77], [inf, -inf])
+    q[1] = 0.0
+    put(1, 7, 1, 1, [0, 127], [inf, nan])
+    for t, values in ((5, [inf, -inf, inf, nan]), (6, [1.0, -inf, -inf, 2.0])):
+        put(2, t, 1, 0, [9, 20, 64, 100], values)
+    pool.k[3].zero_()
+    pool.write(3, 0, pool.k[3], pool.v[3])
+    q[3] = 0.0
+    q[3, :, 0] = 1.0
+    for t, bits in ((33, 25), (49, 40)):
+        put(3, t, 0, 0, [0], [-bits * math.log(2) * math.sqrt(128)])
+        put(3, t, 1, 0, [t], [inf])
+    put(4, 1499, 1, 1, [63], [-inf])
+    put(4, 700, 1, 0, [1], [inf])
+    put(5, 16, 1, 0, [2], [inf])
+    lse = torch.empty((6, 6), device=DEV)
+    out = paged.decode_attention(pool.pages, 0, q, pool.table, pool.device_lens, lse=lse).double()
+    for b in range(6):
+        ref, ref_lse = attend(q[b], pool.k[b], pool.v[b])
+        assert not torch.isfinite(ref).all()
+        assert torch.equal(torch.isnan(out[b]), torch.isnan(ref)), b
+        odd = torch.isinf(ref)
+        assert torch.equal(out[b][odd], ref[odd]) and torch.equal(torch.isinf(out[b]), odd), b
+        fine = torch.isfinite(ref)
+        assert (out[b] - ref)[fine].abs().max() <= 2 * SCORE * 6 and (lse[b] - ref_lse).abs().max() <= SCORE, b
+    assert pool.pages.device_error() == 0
