@@ -58,3 +58,26 @@ def test_decode_infinite_values(page, dtype):
         fine = torch.isfinite(ref)
         assert (out[b] - ref)[fine].abs().max() <= 2 * SCORE * 6 and (lse[b] - ref_lse).abs().max() <= SCORE, b
     assert pool.pages.device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [5, 12, 18, 24, 28.5, 30.5, 33])
+def test_decode_small_weights(bits, dtype):
+    """Every unit has one token of weight 1 and value 0 beside fifteen of weight 2^-bits and values of 0.5 to 1.5, so the result
+    is what the small weights keep.  A weight carries 22 bits, or 2^-42 of the largest where that is more: the scores' SCORE on
+    either side as everywhere, and 15 * 1.5 * 2^-42."""
+    rng = np.random.default_rng([62, int(2 * bits)])
+    n = 1600
+    pool = Pool(rng, [n], 1, 16, dtype)
+    large = torch.arange(n, device=DEV) % 16 == 3
+    pool.k[0].zero_()
+    pool.k[0][~large, 0, 0] = -bits * math.log(2)
+    pool.v[0].copy_(torch.from_numpy(rng.uniform(0.5, 1.5, (n, 1, 128))).to(DEV))
+    pool.v[0][large] = 0.0
+    pool.write(0, 0, pool.k[0], pool.v[0])
+    q = torch.zeros((1, 4, 128), dtype=dtype, device=DEV)
+    q[..., 0] = 1.0
+    out = paged.decode_attention(pool.pages, 0, q, pool.table, pool.device_lens, scale=1.0).double()
+    ref, _ = attend(q[0], pool.k[0], pool.v[0], scale=1.0)
+    assert torch.all((out[0] - ref).abs() <= 2 * SCORE * ref + 15 * 1.5 * 2.0 ** -42)
+    assert pool.pages.device_error() == 0
