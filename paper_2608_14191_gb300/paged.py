@@ -309,18 +309,24 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
 
 
 def copy_pages(pages: Pages, pairs, stream=None):
-    """aatc_pages_copy: page pairs[i][0] to page pairs[i][1] in every layer; pairs int32 [n][2] on the
-    host.  No page may be written twice, or be both read and written."""
+    """aatc_pages_copy: page pairs[i][0] to page pairs[i][1] in every layer; pairs int32 (or equal whole
+    numbers) [n][2] on the host.  No page may be written twice, or be both read and written."""
     where = "aatc_pages_copy"
     _pages(pages, where)
     st = _calls.copy(pages._addr, pages._layers[0], pages.n_layers, pages.layer_bytes, pairs,
                      None if stream is None else stream.cuda_stream)
     if st is None:
-        p = np.ascontiguousarray(pairs, dtype=np.int32)
-        if p.size == 0:
+        given = np.asarray(pairs)
+        if given.size == 0:
             return
-        if p.ndim != 2 or p.shape[1] != 2:
+        if given.ndim != 2 or given.shape[1] != 2:
             _arg_error(where, "pairs must be [n][2]")
+        if given.dtype.kind not in "biuf":
+            _arg_error(where, "pairs must be whole numbers")
+        with np.errstate(invalid="ignore"):
+            p = np.ascontiguousarray(given.astype(np.int32))
+        if not np.array_equal(p, given):      # (the conversion cuts fractions off and wraps what int32 cannot hold)
+            _arg_error(where, "pairs must be page ids: whole numbers of 32 bits")
         st = pages._lib.aatc_pages_copy(pages._addr, pages._layers[0], pages.n_layers, pages.layer_bytes, p.ctypes.data,
                                         p.shape[0], _stream(stream))
     if st:

@@ -196,3 +196,17 @@ def test_places_past_31_bits_are_refused(paged, aatc):
         refused(aatc.AatcError, lambda: paged.gather(p, 0, t, first, 1, stream=S))
     refused(aatc.AatcError, lambda: paged.decode_attention(p, 0, torch.zeros((3, 2, 128), dtype=bf16), t, n, window=2**32 + 5,
                                                            workspace=torch.zeros(1 << 20), stream=S))
+
+
+def test_copy_ids_are_not_wrapped(paged, aatc):
+    """Ids that int32 does not hold, and fractions, are refused, not turned into another page's id."""
+    p = pool(paged)
+    for pairs in (np.array([[2**32 + 3, 1]]), np.array([[1, 2**32 + 3]]), np.array([[-2**32 + 3, 1]]), np.array([[1.7, 3]]),
+                  np.array([[3, math.nan]]), np.array([[math.inf, 3]]), np.array([[2**31 + 2**31 + 1, 3]], np.uint64),
+                  np.array([[2**63 + 3, 1]], np.uint64), [(2**70, 1)], [("1", "2")], torch.tensor([[2**32 + 3, 1]])):
+        refused(aatc.AatcError, lambda: paged.copy_pages(p, pairs, stream=S), what="pairs")
+    # equal whole numbers of other types are taken: only the library refuses these, for page 4, which is written twice
+    for pairs in (np.array([[1.0, 4.0], [2.0, 4.0]]), np.array([[1, 4], [2, 4]], np.uint8), torch.tensor([[1, 4], [2, 4]])):
+        with pytest.raises(aatc.AatcError) as e:
+            paged.copy_pages(p, pairs, stream=S)
+        assert e.value.status == 1 and "pairs" not in str(e.value)
