@@ -128,9 +128,9 @@ class Pages:
             n = self._needs[n_q_heads] = got.value
         return n
 
-    def decode_workspace(self, n_q_heads: int):
+    def decode_workspace(self, n_q_heads: int, stream=None):
         """A workspace for decode_attention: enough for any batch and any lengths."""
-        return torch.empty(max(4, self.decode_workspace_bytes(n_q_heads) // 4), dtype=_F32T, device=self.device)
+        return _made((max(4, self.decode_workspace_bytes(n_q_heads) // 4),), _F32T, self.device, stream)
 
     def device_error(self, clear: bool = False) -> int:
         """Flags that kernels raised (2: a bounded wait timed out, 4: a page id outside the pool, 8: a row,
@@ -177,10 +177,15 @@ def _table(t, where: str, n_rows=None):
     return t.data_ptr(), n, t.stride(0) if n > 1 else m, m
 
 
-def _kept(t, stream):
-    """A tensor made here for a call on `stream`: its memory is not given away before that stream is done with it."""
-    if stream is not None and t.is_cuda:
-        t.record_stream(stream)
+def _made(shape, dtype, device, stream):
+    """An empty tensor for a call on `stream` (None: the current one).  Its memory is that stream's: a block that the
+    current stream got back may still be in use by what is queued there, which `stream` does not wait for.  And the
+    caller may use the tensor on the current stream, so it is not given away again before that is done with it."""
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
     return t
 
 
@@ -196,7 +201,7 @@ def rotate(rope: Rotary, x, positions, out=None, backward: bool = False, stream=
     if not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
     if out is None and isinstance(x, torch.Tensor):
-        out = _kept(torch.empty(x.shape, dtype=x.dtype, device=x.device), stream)
+        out = _made(x.shape, x.dtype, x.device, stream)
     st = _calls.rotate(rope._addr, x, positions, out, backward, None if stream is None else stream.cuda_stream)
     if st is None:
         if not _on_device(x) or x.dtype not in _TYPES:
@@ -223,7 +228,7 @@ def append(pages: Pages, layer: int, k, v, table, index, rows=None, positions=No
     if rope is not None and not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
     if q is not None and q_out is None and _on_device(q):
-        q_out = _kept(torch.empty(q.shape, dtype=q.dtype, device=q.device), stream)
+        q_out = _made(q.shape, q.dtype, q.device, stream)
     base, ro = pages.layer(layer, where), None if rope is None else rope._addr
     st = _calls.append(pages._addr, base, pages._flags, pages.dtype, pages.n_kv_heads, k, v, table, index, rows, positions, ro,
                        q, q_out, None if stream is None else stream.cuda_stream)
@@ -268,7 +273,7 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
     _pages(pages, where)
     base = pages.layer(layer, where)
     if out is None and _on_device(q):
-        out = _kept(torch.empty(q.shape, dtype=_F32T, device=q.device), stream)
+        out = _made(q.shape, _F32T, q.device, stream)
     if prior is None:
         prior = (None, None)
     elif not isinstance(prior, (tuple, list)) or len(prior) != 2 or prior[0] is None or prior[1] is None:
@@ -297,7 +302,7 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
         if batch == 0:
             return out
         if workspace is None:             # (the library refuses one that is too small)
-            workspace = _kept(pages.decode_workspace(n_q), stream)
+            workspace = pages.decode_workspace(n_q, stream)
         elif not _on_device(workspace) or not workspace.is_contiguous():
             _arg_error(where, "workspace must be a contiguous device tensor")
         st = pages._lib.aatc_paged_decode_attention(pages._addr, base, tp, ts, tm, lp, batch, ctypes.byref(qh), n_q,
@@ -344,8 +349,8 @@ def gather(pages: Pages, layer: int, table, first: int, n_tokens: int, lens=None
         if not _on_device(table) or n_tokens < 0:
             _arg_error(where, "table must be a device tensor, n_tokens not negative")
         shape = (table.shape[0], n_tokens, pages.n_kv_heads, HEAD_DIM)
-        k = _kept(torch.empty(shape, dtype=pages.dtype, device=pages.device), stream)
-        v = _kept(torch.empty(shape, dtype=pages.dtype, device=pages.device), stream)
+        k = _made(shape, pages.dtype, pages.device, stream)
+        v = _made(shape, pages.dtype, pages.device, stream)
     elif isinstance(out, (tuple, list)) and len(out) == 2:
         k, v = out
     else:

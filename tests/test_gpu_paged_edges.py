@@ -81,3 +81,39 @@ def test_decode_small_weights(bits, dtype):
     ref, _ = attend(q[0], pool.k[0], pool.v[0], scale=1.0)
     assert torch.all((out[0] - ref).abs() <= 2 * SCORE * ref + 15 * 1.5 * 2.0 ** -42)
     assert pool.pages.device_error() == 0
+
+
+def test_results_of_a_given_stream_are_in_its_own_memory():
+    """A result that is made for a call on another stream does not lie in a block that the current stream got back just
+    before (what is queued there may still use it), and the values come out with work queued on both."""
+    rng = np.random.default_rng(63)
+    pool = Pool(rng, [300, 47], 2, 16, torch.bfloat16)
+    rope = paged.Rotary(64, 10000.0, device=DEV)
+    q = normal(rng, (2, 8, 128), torch.bfloat16)
+    x = normal(rng, (4000, 8, 128), torch.bfloat16)
+    places = torch.tensor([300, 47], dtype=torch.int32, device=DEV)
+    kv = normal(rng, (2, 2, 128), torch.bfloat16)
+    far = torch.arange(4000, dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    calls = {
+        "rotate": lambda stream: (paged.rotate(rope, x, far, stream=stream),),
+        "append": lambda stream: (paged.append(pool.pages, 0, kv, kv, pool.table, places, rope=rope, q=q, stream=stream),),
+        "decode": lambda stream: (paged.decode_attention(pool.pages, 0, q, pool.table, pool.device_lens, stream=stream),),
+        "gather": lambda stream: paged.gather(pool.pages, 0, pool.table, 0, 40, stream=stream),
+    }
+    for name, call in calls.items():
+        want = call(None)
+        shapes = [(w.shape, w.dtype) for w in want]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            held = [torch.empty(s, dtype=d, device=DEV) for s, d in shapes for _ in range(4)]
+            blocks = [(h.data_ptr(), h.data_ptr() + h.nbytes) for h in held]
+            torch.cuda._sleep(2_000_000)                          # about a millisecond of the current stream's time
+            for h in held:
+                h.fill_(7.0)
+            del held, h
+            got = call(side)
+            assert not any(a < g.data_ptr() + g.nbytes and g.data_ptr() < b for g in got for a, b in blocks), name
+            torch.cuda.synchronize()
+            assert all(torch.equal(g, w) for g, w in zip(got, want)), name
+    assert pool.pages.device_error() == 0
