@@ -600,9 +600,10 @@ __global__ void __launch_bounds__(kDecodeThreads, 1)
           stage = 0;
           ++round;
         }
-        idle_since = 0;
       }
-      if (!__any_sync(0xffffffffu, can)) {           // (a consumer that stopped, stops this too)
+      if (__any_sync(0xffffffffu, can)) {            // (whichever lane went on: the others may have nothing to do for long)
+        idle_since = 0;
+      } else {                                       // (a consumer that stopped, stops this too)
         if (__any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&s_abort))) break;
         const uint64_t now = ptx::globaltimer_ns();
         if (idle_since == 0) idle_since = now;

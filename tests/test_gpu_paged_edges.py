@@ -117,3 +117,37 @@ def test_results_of_a_given_stream_are_in_its_own_memory():
             torch.cuda.synchronize()
             assert all(torch.equal(g, w) for g, w in zip(got, want)), name
     assert pool.pages.device_error() == 0
+
+
+def test_decode_longer_than_its_waits():
+    """A call of some three seconds (65535 sequences that share 896000 places of 64 pages) is not taken for one that stands
+    still: its waits are bounded at one and two seconds each, of no progress.  A lane of the kernel adds up to 56000
+    weights between 0.01 and 100 one after the other: relative 56000 * 2^-24 of the sum and of the outputs' sums."""
+    rng = np.random.default_rng(64)
+    batch, places, n_q = 65535, 3500, 2
+    pages = paged.Pages(1, 64, 1, 256, torch.bfloat16, DEV)
+    pages.data.copy_(torch.from_numpy(rng.standard_normal(pages.data.shape)))
+    pages.data[:, :, 1] = pages.data[:, :, 1].clamp(-1, 1) / 2 + 1
+    host = rng.integers(0, 64, places)
+    table = torch.from_numpy(host).to(DEV, torch.int32)[None].expand(batch, -1)
+    q = normal(rng, (1, n_q, 128), torch.bfloat16)
+    lens = torch.full((batch,), places * 256, dtype=torch.int32, device=DEV)
+    out = torch.full((batch, n_q, 128), math.nan, device=DEV)
+    lse = torch.full((batch, n_q), math.nan, device=DEV)
+    workspace = pages.decode_workspace(n_q)
+    begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    begin.record()
+    paged.decode_attention(pages, 0, q.expand(batch, -1, -1), table, lens, out=out, lse=lse, workspace=workspace)
+    end.record()
+    end.synchronize()
+    assert pages.device_error() == 0
+    assert begin.elapsed_time(end) > 2000                          # (or it does not reach what it is for)
+    k, v = (pages.data[0, :, i, 0].double().reshape(-1, 128) for i in (0, 1))
+    times = torch.from_numpy(np.bincount(host, minlength=64)).to(DEV).repeat_interleave(256).double()
+    s = q[0].double() @ k.T / math.sqrt(128)
+    assert s.abs().max() < math.log(100)
+    weights = times * torch.exp(s)
+    ref, ref_lse = weights @ v / weights.sum(1, keepdim=True), weights.sum(1).log()
+    chain = 56000 * 2.0 ** -24
+    assert torch.all((lse - ref_lse).abs() <= SCORE + chain)
+    assert torch.all((out - ref).abs() <= (2 * SCORE + 2 * chain) * 1.5)
