@@ -530,7 +530,7 @@ typedef struct {
  * same factor): the gradient with respect to x, given the gradient of out.  fp32 arithmetic, one rounding.
  *   positions : device int32 [n_tokens], of any sign
  *   x, out    : device, token and head strides in elements; out may be x itself (same strides), and
- *               must not overlap it otherwise
+ *               must not overlap it otherwise; no two heads of out may overlap (x may be broadcast)
  * Errors: AATC_ERR_INVALID_ARG.  n_tokens == 0 is a no-op.
  */
 aatc_status_t aatc_rotate(const aatc_rotary_t* rope, int32_t dtype, const void* x, int64_t x_token_stride,
@@ -549,6 +549,7 @@ aatc_status_t aatc_rotate(const aatc_rotary_t* rope, int32_t dtype, const void* 
  *   k, v      : device [n_tokens][n_kv_heads][128]
  *   rope      : NULL: keys are written as they are (q must then be NULL too)
  *   q, q_out  : device [n_tokens][n_q_heads][128], or NULL both; q_out contiguous, or q itself
+ *               (then no two of its heads may overlap)
  * Errors: AATC_ERR_INVALID_ARG.  n_tokens == 0 is a no-op.
  */
 typedef struct {

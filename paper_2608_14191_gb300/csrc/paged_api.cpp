@@ -32,6 +32,21 @@ bool heads_ok(const aatc_heads_t* h) {
   return h && h->x && aligned16(h->x) && h->token_stride % 8 == 0 && h->head_stride % 8 == 0;
 }
 
+// Whether no two of the n_tokens x n_heads heads at these strides overlap, as the ones that a call writes must not (of a
+// tensor that is broadcast, they all do; and where it is turned in place, some would be turned twice).
+bool apart(int64_t token_stride, int64_t head_stride, int64_t n_tokens, int64_t n_heads) {
+  using wide = __int128;
+  const wide a = token_stride < 0 ? -static_cast<wide>(token_stride) : token_stride;
+  const wide b = head_stride < 0 ? -static_cast<wide>(head_stride) : head_stride;
+  if ((n_tokens > 1 && a < D) || (n_heads > 1 && b < D)) return false;
+  if (n_tokens <= 1 || n_heads <= 1 || a >= (n_heads - 1) * b + D || b >= (n_tokens - 1) * a + D) return true;
+  for (int64_t i = 1; i < n_heads; ++i) {            // neither within the other: the heads nearest to i heads on
+    const wide j = i * b / a, off = i * b - j * a;
+    if ((j < n_tokens && off < D) || (j + 1 < n_tokens && a - off < D)) return false;
+  }
+  return true;
+}
+
 paged::Heads heads(const aatc_heads_t* h) { return {h->x, h->token_stride, h->head_stride}; }
 
 bool rope_ok(const aatc_rotary_t* r) {
@@ -139,6 +154,7 @@ aatc_status_t aatc_rotate(const aatc_rotary_t* rope, int32_t dtype, const void* 
   const aatc_heads_t in = {x, x_token_stride, x_head_stride}, res = {out, out_token_stride, out_head_stride};
   if (!rope_ok(rope) || (dtype != AATC_BF16 && dtype != AATC_F16) || !heads_ok(&in) || !heads_ok(&res) || !positions ||
       !aligned4(positions) || n_tokens < 0 || n_heads < 1 || n_heads > 65536 ||
+      !apart(out_token_stride, out_head_stride, n_tokens, n_heads) ||
       (x == out && (x_token_stride != out_token_stride || x_head_stride != out_head_stride)))
     return AATC_ERR_INVALID_ARG;
   paged::AppendArgs a = {};
@@ -164,7 +180,9 @@ aatc_status_t aatc_paged_append(const aatc_pages_t* desc, void* pages, const int
       !aligned4(rows) || !aligned4(positions) || !aligned4(dev_flags) || n_tokens < 0 || !heads_ok(k) || !heads_ok(v) ||
       (rope && !rope_ok(rope)) || (q != nullptr) != (q_out != nullptr))
     return AATC_ERR_INVALID_ARG;
-  if (q && (!rope || !heads_ok(q) || !aligned16(q_out) || n_q_heads < 1 || n_q_heads > 65536)) return AATC_ERR_INVALID_ARG;
+  if (q && (!rope || !heads_ok(q) || !aligned16(q_out) || n_q_heads < 1 || n_q_heads > 65536 ||
+            (q_out == q->x && !apart(q->token_stride, q->head_stride, n_tokens, n_q_heads))))
+    return AATC_ERR_INVALID_ARG;
   paged::AppendArgs a = {};
   a.pool = pool(desc, pages, table, table_stride, max_pages, dev_flags);
   if (rope) a.turn = turn(rope, false);

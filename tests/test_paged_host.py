@@ -210,3 +210,26 @@ def test_copy_ids_are_not_wrapped(paged, aatc):
         with pytest.raises(aatc.AatcError) as e:
             paged.copy_pages(p, pairs, stream=S)
         assert e.value.status == 1 and "pairs" not in str(e.value)
+
+
+def test_overlapping_results_are_refused(paged, aatc):
+    """Results whose heads overlap, among them a broadcast tensor turned in place; strides that only cross are taken (the launch
+    itself then fails here)."""
+    rope, p = paged.Rotary(64, device="cpu"), torch.zeros(6, dtype=i32)
+    x, flat = torch.zeros((6, 4, 128), dtype=bf16), torch.zeros(1 << 16, dtype=bf16)
+    one = x[:1].expand(6, 4, 128)
+    bad = [one, x[:, :1].expand(6, 4, 128)] + [flat.as_strided((6, 4, 128), s + (1,)) for s in (
+        (128, 128), (512, 64), (64, 1024), (256, 384), (384, 128), (128, 640), (1000, 504))]
+    for out in bad:
+        refused(aatc.AatcError, lambda: paged.rotate(rope, x, p, out=out, stream=S))
+        refused(aatc.AatcError, lambda: paged.rotate(rope, out, p, out=out, stream=S))
+    pages, t = pool(paged), torch.zeros((6, 4), dtype=i32)
+    for q in bad:
+        refused(aatc.AatcError, lambda: paged.append(pages, 0, x[:, :2], x[:, :2], t, p, rope=rope, q=q, q_out=q, stream=S))
+    good = [(x.clone(), one), (x.clone(), x[:, :1].expand(6, 4, 128)), (x[:1].expand(1, 4, 128), x[:1])]
+    good += [(y, y) for y in (flat.as_strided(n + (128,), s + (1,)) for n, s in (
+        ((6, 4), (512, 128)), ((6, 4), (128, 768)), ((2, 3), (384, 256)), ((3, 2), (256, 384)), ((2, 1), (128, 0)), ((1, 4), (0, 136))))]
+    for out, src in good:
+        with pytest.raises(aatc.AatcError) as e:
+            paged.rotate(rope, src, p[:len(src)], out=out, stream=S)
+        assert e.value.status != 1
