@@ -612,7 +612,8 @@ aatc_status_t aatc_pages_copy(const aatc_pages_t* desc, void* pages, int32_t n_l
  * Gather tokens [first, first + n_tokens) of each of n_rows sequences out of their pages:
  *   k_out, v_out : device [n_rows][n_tokens][n_kv_heads][128], contiguous (what aatc_encode takes)
  *   lens         : device int32 [n_rows] or NULL; tokens at or past their sequence's length are written
- *                  as zeros and their pages are not read
+ *                  as zeros and their pages are not read (a length outside the table is flagged, and taken as 0
+ *                  or as the whole table)
  * Errors: AATC_ERR_INVALID_ARG, AATC_ERR_CAPACITY (first + n_tokens > max_pages * page_size, or past 2^31 - 1).
  * n_tokens or n_rows == 0 is a no-op.
  */

@@ -1090,6 +1090,8 @@ __global__ void __launch_bounds__(256) aatc_paged_gather_kernel(const GatherArgs
 #pragma unroll
   for (int k = 0; k < kCopyVecs; ++k)
     if (to[k]) *to[k] = x[k];
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.lens && (n < 0 || n > static_cast<int64_t>(p.max_pages) << p.page_shift))
+    raise(p.err, kBadRow);
 }
 
 }  // namespace

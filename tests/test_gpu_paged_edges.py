@@ -151,3 +151,20 @@ def test_decode_longer_than_its_waits():
     chain = 56000 * 2.0 ** -24
     assert torch.all((lse - ref_lse).abs() <= SCORE + chain)
     assert torch.all((out - ref).abs() <= (2 * SCORE + 2 * chain) * 1.5)
+
+
+@pytest.mark.parametrize("n", [1, 40, 5000])
+def test_gather_flags_lengths_outside_the_table(n):
+    """Lengths below 0 and past the table are flagged, as in the decode; they count as 0 and as the whole table."""
+    rng = np.random.default_rng([65, n])
+    pool = Pool(rng, [n, n, n], 2, 16, torch.float16)
+    table = pool.table[:, :-(-n // 16)].contiguous()              # (no wider than the sequences)
+    room = table.shape[1] * 16
+    dev = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    for lens, flag in ((dev(n, 0, room), 0), (dev(n, -1, n), 8), (dev(room + 1, 0, n), 8), (dev(0, n, 2**31 - 1), 8), (dev(-2**31, n, n), 8)):
+        k, v = paged.gather(pool.pages, 0, table, 0, n, lens=lens)
+        assert pool.pages.device_error(clear=True) == flag
+        for r, length in enumerate(lens.tolist()):
+            live = max(0, min(length, n))
+            for got, x in ((k, pool.k), (v, pool.v)):
+                assert torch.equal(got[r, :live], x[r][:live]) and torch.all(got[r, live:] == 0)
