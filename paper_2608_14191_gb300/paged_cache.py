@@ -147,7 +147,7 @@ class PagedSequences:
         rows = np.repeat(np.fromiter(counts, np.int32, len(counts)), list(counts.values()))
         index = [np.arange(old, old + counts[row], dtype=np.int32) for row, old, _ in take]
         index = np.concatenate(index) if index else np.zeros(0, np.int32)
-        return (self._staged(x).to(self.pages.device, non_blocking=True) for x in (rows, index))
+        return tuple(self._staged(x).to(self.pages.device, non_blocking=True) for x in (rows, index))
 
     def drop_front(self, row: int, tokens: int):
         """Takes the first `tokens` tokens (whole pages) away from a sequence."""

@@ -144,6 +144,22 @@ def test_bookkeeping_refusals(books):
     b.check()
 
 
+def test_grow_returns_a_pair(books, monkeypatch):
+    """(rows, index) are there when the call returns, staged with the call's own uploads, and can be read more than once."""
+    b = books(20, 3, 64, 8)
+    b.s.add()
+    b.s.add()
+    staged = []
+    monkeypatch.setattr(b.s, "_staged", lambda x, real=b.s._staged: staged.append(len(np.atleast_1d(x))) or real(x))
+    got = b.s.grow({0: 3, 1: 2})
+    assert len(staged) == 4                                       # table, lengths, rows, index
+    assert isinstance(got, tuple) and len(got) == 2
+    for _ in range(2):
+        rows, index = got
+        assert rows.tolist() == [0, 0, 0, 1, 1] and index.tolist() == [0, 1, 2, 0, 1]
+        assert rows.dtype == index.dtype == torch.int32
+
+
 @pytest.mark.gpu
 def test_tail_cache(aatc):
     """Ragged sequences, coded as the window allows, forked on the way: every step's attention against 64 bits over
