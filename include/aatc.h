@@ -571,8 +571,8 @@ aatc_status_t aatc_paged_append(const aatc_pages_t* desc, void* pages, const int
  * A sequence of no tokens gives out = 0, lse = -infinity.  A prior (prior_out, prior_lse) of another set
  * of tokens, as this call or aatc_decode_attention_lse writes it, joins the same softmax.  The lengths are read on
  * the device, so a captured call serves sequences that grow.  The tokens of all sequences are dealt out evenly
- * over the SMs in one launch and the pieces joined in a second (where the table or the window is wider than 256
- * tokens); fp32 softmax and sums, fp32 results.
+ * over the SMs in one launch and the pieces joined in a second (where the table and the window hold 272 tokens or
+ * more, or the batch is over 1536); fp32 softmax and sums, fp32 results.
  *   lens      : device int32 [batch], 0 .. max_pages * page_size
  *   q         : device [batch][n_q_heads][128], token_stride between sequences
  *   slopes    : device fp32 [n_q_heads] or NULL

@@ -191,11 +191,11 @@ constexpr int kStages = 2;          // units of a consumer on their way: keys an
                                     // 86 with two, as with three when those fitted)
 constexpr int kGap = 8;             // units' time that a segment costs beside its units (61 ragged sequences: 5 49.8 us,
                                     // 8 49.7, 12 51.3; 600 of up to 40 tokens 24.7, 24.1, 22.4)
-// Where no segment can have more units than this (by the table's width or the window), the CTAs' parts of the line are
+// Where every segment has fewer tokens than this (by the table's width or the window), the CTAs' parts of the line are
 // moved to whole segments and there is no second launch.  300 sequences of 1 to 40 tokens x 4 kv-heads: 10.7 us against 17.1
 // with it; one sequence x 8 kv-heads of 100 tokens 6.0 against 7.0, of 250 7.3 against 7.1 (and a launch less for the host, 2
 // us), of 500 9.5 against 7.3.
-constexpr int kWholeUnits = 16;
+constexpr int kWholeTokens = 17 * kUnit;
 // Pieces that a segment can have from which sixteen warps join them, not four: 131072 tokens x 1 kv-head 21.2 us against 23.0;
 // but 4000 tokens x 1 kv-head (at most 35 pieces) 9.2 against 7.6.
 constexpr int kManyPieces = 64;
@@ -1112,11 +1112,11 @@ cudaError_t launch_decode(int dtype, const DecodeArgs& a, cudaStream_t st) {
   const int ctas = std::max(1, a.num_sms);
   const int64_t seqs_units = (static_cast<int64_t>(a.pool.max_pages) << a.pool.page_shift) / kUnit + 1 + kGap;
   const int n_seg = a.pool.n_kv * ((a.group + kSegHeads - 1) / kSegHeads);
-  // units of the longest segment that the table's width and the window let be
-  const int64_t tokens_most = static_cast<int64_t>(a.pool.max_pages) << a.pool.page_shift;
-  const int64_t units_most = (a.window > 0 ? std::min<int64_t>(tokens_most, a.window) : tokens_most) / kUnit + 2;
+  // tokens and units of the longest segment that the table's width and the window let be
+  const int64_t room = static_cast<int64_t>(a.pool.max_pages) << a.pool.page_shift;
+  const int64_t tokens_most = a.window > 0 ? std::min<int64_t>(room, a.window) : room, units_most = tokens_most / kUnit + 2;
   DecodeArgs args = a;
-  args.whole = units_most <= kWholeUnits + 2 && a.batch <= kChunk;
+  args.whole = tokens_most < kWholeTokens && a.batch <= kChunk;
   const bool narrow = seqs_units * n_seg < ((1ll << 31) - (1 << 16)) / a.batch;
   const bool bf16 = dtype == AATC_BF16;
   const auto kernel = narrow ? (bf16 ? aatc_paged_decode_kernel<__nv_bfloat16, int> : aatc_paged_decode_kernel<__half, int>)

@@ -168,3 +168,33 @@ def test_gather_flags_lengths_outside_the_table(n):
             live = max(0, min(length, n))
             for got, x in ((k, pool.k), (v, pool.v)):
                 assert torch.equal(got[r, :live], x[r][:live]) and torch.all(got[r, live:] == 0)
+
+
+@pytest.mark.parametrize("batch", [1, 100, 385])
+@pytest.mark.parametrize("room,window", [(256, 0), (264, 0), (272, 0), (640, 255), (640, 256), (640, 257), (640, 271), (640, 272), (256, 300)])
+def test_decode_around_whole_segments(room, window, batch):
+    """Tables and windows of fewer than 272 tokens, whose segments go whole to one CTA, and wider ones, whose pieces go through the
+    workspace; the lengths let windows begin anywhere in a unit."""
+    rng = np.random.default_rng([66, room, window, batch])
+    lens = rng.integers(0, room + 1, batch)
+    lens[rng.integers(0, batch)] = room
+    pages = paged.Pages(1, batch * room // 8, 2, 8, torch.bfloat16, DEV)
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(DEV, torch.int32)  # noqa: E731
+    table = dev(rng.permutation(pages.n_pages).reshape(batch, -1))
+    index = np.concatenate([np.arange(n) for n in lens])
+    k, v = (normal(rng, (len(index), 2, 128), torch.bfloat16) for _ in range(2))
+    paged.append(pages, 0, k, v, table, dev(index), rows=dev(np.repeat(np.arange(batch), lens)))
+    q = normal(rng, (batch, 6, 128), torch.bfloat16)
+    workspace = pages.decode_workspace(6).fill_(-3.0)
+    lse = torch.empty((batch, 6), device=DEV)
+    out = paged.decode_attention(pages, 0, q, table, dev(lens), lse=lse, window=window, workspace=workspace)
+    start = np.concatenate([[0], np.cumsum(lens)])
+    for b in range(batch):
+        part = slice(int(start[b]), int(start[b + 1]))
+        ref, ref_lse = attend(q[b], k[part], v[part], window=window)
+        assert (out[b] - ref).abs().max() <= 2 * SCORE * 6, b
+        assert lens[b] == 0 or (lse[b] - ref_lse).abs().max() <= SCORE, b
+    whole = min(room, window or room) < 272
+    pieces = workspace[:-4 * torch.cuda.get_device_properties(0).multi_processor_count]
+    assert bool((pieces == -3.0).all()) == whole
+    assert pages.device_error() == 0
