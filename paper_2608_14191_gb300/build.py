@@ -1,7 +1,9 @@
 """Build the in-tree CUDA library ``libaatc.so`` for sm_103a with nvcc (no cmake).
 
 Each translation unit compiles in parallel; the shared object lands next to this file, and with it
-``_calls.so``, the Python extension through which the binding makes the paged calls.
+``_calls``, the Python extension through which the binding makes the paged calls (under the name that this
+interpreter's modules have, so that another one does not load it).  The library needs no Python: where the
+interpreter's headers are missing it is built alone.
 """
 from __future__ import annotations
 
@@ -17,7 +19,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libaatc.so")
-CALLS = os.path.join(HERE, "_calls.so")
+CALLS = os.path.join(HERE, "_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["planner.cpp", "planfile.cpp", "capi.cpp", "encode.cu", "decode.cu", "prefill.cu", "group.cu", "paged_api.cpp", "paged.cu",
            "selftest.cu"]
 CALLS_SOURCE = "pycalls.cpp"
@@ -36,11 +38,17 @@ def _flags():
                    "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
 
 
+def _python_include() -> str | None:
+    """The directory of the interpreter's headers, if they are installed."""
+    path = sysconfig.get_paths()["include"]
+    return path if os.path.exists(os.path.join(path, "Python.h")) else None
+
+
 def _compile(src: str, verbose: bool) -> str:
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
     cmd = [_nvcc()] + _flags() + ["-c", os.path.join(CSRC, src), "-o", obj]
     if src == CALLS_SOURCE:
-        cmd += ["-I" + sysconfig.get_paths()["include"]]
+        cmd += ["-I" + _python_include()]
     if src.endswith(".cu") and verbose:
         cmd += ["-Xptxas", "-v"]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -54,15 +62,19 @@ def _compile(src: str, verbose: bool) -> str:
 def build(verbose: bool = False, force: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "aatc.h")]
-    if not force and os.path.exists(LIB) and os.path.exists(CALLS):
+    with_calls = _python_include() is not None
+    built = [LIB] + ([CALLS] if with_calls else [])
+    if not force and all(os.path.exists(p) for p in built):
         newest = max(os.path.getmtime(p) for p in deps)
-        if os.path.getmtime(LIB) >= newest and os.path.getmtime(CALLS) >= newest:
+        if min(os.path.getmtime(p) for p in built) >= newest:
             return LIB
-    sources = SOURCES + [CALLS_SOURCE]
-    with cf.ThreadPoolExecutor(max_workers=len(sources)) as ex:
-        objs = list(ex.map(lambda s: _compile(s, verbose), sources))
-    _link(LIB, objs[:-1] + ["-lpthread", "-ldl", "-lrt"])
-    _link(CALLS, objs[-1:] + ["-L" + HERE, "-l:" + os.path.basename(LIB), "-Xlinker", "-rpath,$ORIGIN"])
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        calls = ex.submit(_compile, CALLS_SOURCE, verbose) if with_calls else None
+        _link(LIB, list(ex.map(lambda s: _compile(s, verbose), SOURCES)) + ["-lpthread", "-ldl", "-lrt"])
+        if calls is None:
+            sys.stderr.write("Python's headers are missing: the extension of the paged calls is not built\n")
+        else:
+            _link(CALLS, [calls.result(), "-L" + HERE, "-l:" + os.path.basename(LIB), "-Xlinker", "-rpath,$ORIGIN"])
     return LIB
 
 

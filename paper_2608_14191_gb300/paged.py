@@ -19,7 +19,11 @@ import torch
 from . import HEAD_DIM, _arg_error, _check, _dev_tensor, _on_device, _stream, load
 
 load()                  # (the extension is linked to the library)
-from . import _calls  # noqa: E402
+try:
+    from . import _calls  # noqa: E402
+except ImportError as e:
+    raise ImportError("the extension _calls is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'` "
+                      "(it needs Python's headers)") from e
 
 _calls.setup(torch.int32, torch.float32, torch.bfloat16, torch.float16, torch._C._cuda_getCurrentRawStream,
              torch._C._cuda_getDevice)
