@@ -472,7 +472,7 @@ aatc_status_t aatc_bf16_decode_attention(const void* K, const void* V, const voi
  * read on the device, so the library cannot refuse a bad one before the launch: every kernel
  * checks each id and length that it reads, skips what lies outside the pool, and raises a bit of
  * the caller's flags (dev_flags: device int32, ORed into, may be NULL):
- *   bit 1 (2): a bounded wait inside a kernel timed out;  bit 2 (4): a page id outside [0, n_pages);
+ *   bit 1 (2): a bounded wait inside a kernel timed out (the call's results are not to be used);  bit 2 (4): a page id outside [0, n_pages);
  *   bit 3 (8): a row, index or length outside the table.
  * Base pointers are 16-byte aligned, and strides (in elements) of keys, values and queries are
  * multiples of 8; the 128 values of one head are contiguous.
@@ -569,7 +569,8 @@ aatc_status_t aatc_paged_append(const aatc_pages_t* desc, void* pages, const int
  *   over 0 <= t < n, and t >= n - window if window > 0;
  *   lse = ln sum_t exp(s_t), out = sum_t exp(s_t - lse) v_t.
  * A sequence of no tokens gives out = 0, lse = -infinity.  A prior (prior_out, prior_lse) of another set
- * of tokens, as this call or aatc_decode_attention_lse writes it, joins the same softmax.  The lengths are read on
+ * of tokens, as this call or aatc_decode_attention_lse writes it, joins the same softmax; its scores are to be
+ * of the same kind (aatc_decode_attention_lse has the scale 1 / sqrt(128), and no cap and no slopes).  The lengths are read on
  * the device, so a captured call serves sequences that grow.  The tokens of all sequences are dealt out evenly
  * over the SMs in one launch and the pieces joined in a second (where the table and the window hold 272 tokens or
  * more, or the batch is over 1536); fp32 softmax and sums, fp32 results.
@@ -610,7 +611,8 @@ aatc_status_t aatc_pages_copy(const aatc_pages_t* desc, void* pages, int32_t n_l
 
 /*
  * Gather tokens [first, first + n_tokens) of each of n_rows sequences out of their pages:
- *   k_out, v_out : device [n_rows][n_tokens][n_kv_heads][128], contiguous (what aatc_encode takes)
+ *   k_out, v_out : device [n_rows][n_tokens][n_kv_heads][128], contiguous, of the pages' type (of bf16 pages what
+ *                  aatc_encode takes)
  *   lens         : device int32 [n_rows] or NULL; tokens at or past their sequence's length are written
  *                  as zeros and their pages are not read (a length outside the table is flagged, and taken as 0
  *                  or as the whole table)

@@ -200,7 +200,8 @@ def _pages(pages, where: str):
 
 def rotate(rope: Rotary, x, positions, out=None, backward: bool = False, stream=None):
     """aatc_rotate: x [tokens][heads][128] (bf16 or f16, strided) turned by positions (int32 [tokens]).
-    out: None for a new tensor, or x itself.  backward: the gradient with respect to x, given out's."""
+    out: None for a new tensor, x itself, or another tensor of its type whose heads do not overlap.  backward: the
+    gradient with respect to x, given out's; autograd does not record the call."""
     where = "aatc_rotate"
     if not isinstance(rope, Rotary):
         _arg_error(where, "rope must be a Rotary")
@@ -270,8 +271,8 @@ def decode_attention(pages: Pages, layer: int, q, table, lens, out=None, lse=Non
                      cap: float = 0.0, window: int = 0, slopes=None, workspace=None, stream=None):
     """aatc_paged_decode_attention: q [batch][n_q_heads][128] (the pages' type) over the first lens[b]
     tokens (int32 [batch]) of each row of the table -> fp32 [batch][n_q_heads][128].  lse: fp32
-    [batch][n_q_heads], written; prior: (out, lse) of another set of tokens that joins the softmax; scale:
-    1 / sqrt(128) by default; cap: scores become cap tanh(score / cap); window: only the last ones; slopes:
+    [batch][n_q_heads], written; prior: (out, lse) of another set of tokens that joins the softmax, taken with the
+    same scores (the packed decode has the default scale, and no cap and no slopes); scale: 1 / sqrt(128) by default; cap: scores become cap tanh(score / cap); window: only the last ones; slopes:
     fp32 [n_q_heads], slope (t - (len - 1)) is added to the score of token t."""
     where = "aatc_paged_decode_attention"
     _pages(pages, where)
@@ -344,8 +345,8 @@ def copy_pages(pages: Pages, pairs, stream=None):
 
 def gather(pages: Pages, layer: int, table, first: int, n_tokens: int, lens=None, out=None, stream=None):
     """aatc_paged_gather: tokens [first, first + n_tokens) of every row of the table, contiguous:
-    (K, V), each [rows][n_tokens][n_kv_heads][128] as aatc_encode takes them.  lens: int32 [rows];
-    tokens past their sequence's length come out as zeros."""
+    (K, V), each [rows][n_tokens][n_kv_heads][128] (bf16 pages: as aatc_encode takes them; f16 it does not take).
+    lens: int32 [rows]; tokens past their sequence's length come out as zeros."""
     where = "aatc_paged_gather"
     _pages(pages, where)
     base = pages.layer(layer, where)

@@ -184,7 +184,9 @@ class PagedTailCache:
     A step: `begin` (how many new tokens each sequence has), then for every layer `append` and, where each sequence
     has one new token, `attend`, then `end`, which codes old tokens.  A sequence keeps at least `window` tokens in
     full precision; whenever all have `step` more, the oldest `step` of each go to the packed cache.
-    rope: a `paged.Rotary` for the model's positions, or None where keys and queries come turned already."""
+    rope: a `paged.Rotary` for the model's positions, or None where keys and queries come turned already.
+    Scores have the packed decode's scale, no cap and no slopes, and keys and values are bf16.  `coded` is one number:
+    a row without tokens keeps everything from being coded, and rows do not leave or enter once it is above 0."""
 
     def __init__(self, plan, batch: int, max_tokens: int, device="cuda", window: int = 128, step: int = 16,
                  page_size: int = 16, tail_tokens: int | None = None, n_pages: int | None = None, rope=None):
