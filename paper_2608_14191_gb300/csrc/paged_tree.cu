@@ -72,7 +72,7 @@ __device__ __forceinline__ const T* token_at(const Pool& p, int b, int h, int ki
 //
 // What bounds it (GB300): 64 queries x 32 heads over 131072 tokens x 8 kv-heads take 109 to 120 us, 4.5 TB/s and 1.2 PFLOP/s, where the
 // memory alone needs 79 and the same kernel without MMAs and softmax takes 94 to 100: a pair's tile costs 1.9 us of softmax and MMAs in
-// turn, 1.5 of memory.  26 queries x 28 heads of 16 sequences over 8192 tokens (f16) 66 us; 37 ragged sequences with capped scores 69
+// turn, 1.5 of memory.  26 queries x 28 heads of 16 sequences over 8192 tokens (f16) 66 us; 37 ragged sequences with capped scores 73
 // (61 without the cap's exponential and half a reciprocal a score): a segment's begin and end, some 7 us for queries, first tiles, results;
 // 8 queries over 1001 tokens 13.4 us, of which 6 until the first tile is there and 3 the second launch.
 //
@@ -546,24 +546,19 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     const int tid = threadIdx.x - 32 * kSoftmaxWarp, warp = ptx::warp_uniform(tid / 32), slot = warp / 4, r = tid % kSlotRows;
     const uint32_t lanes = static_cast<uint32_t>(32 * (warp % 4)) << 16;
     const uint32_t col_s = tmem + lanes + kColS + 128 * slot, col_o = tmem + lanes + kColO;
-    // scores after c, which is above 0, ascend with S: what caps do, and other scales, is done to S first
-    const bool in_place = kCap || !(a.scale > 0.0f);
+    // scores after c, which is above 0, ascend with S: other scales are done to S first
+    const bool in_place = !(a.scale > 0.0f);
     const float c = in_place ? 1.0f : a.scale * kLog2e;
     const uint64_t c2 = ptx::f2_pack(c, c);
     const float cap_in = (kCap ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap_out = a.cap * kLog2e;
-    // cap tanh y = cap - 2 cap / (e^(2 y) + 1), within 2^-22 of the cap: a score's error is an absolute one
-    auto capped = [&](uint32_t s) {
-      return __float_as_uint(fmaf(-2.0f * cap_out, reciprocal(exp2_of(__uint_as_float(s) * cap_in) + 1.0f), cap_out));
-    };
     constexpr uint32_t kExponent = Half16<T>::kFormat ? 0x7F807F80u : 0x7C007C00u, kOne = Half16<T>::kFormat ? 0x00800080u : 0x04000400u;
-    // Capped scores lie within 2^+-cap_out: in bf16, whose weights and sums have that range, 0 is reference enough, and one pass does.
-    const bool fixed = kCap && Half16<T>::kShift == 0.0f && cap_out <= 100.0f;
-    // two scores with one reciprocal (e^(2 y) up to 2^60, where the cap is reached)
-    auto capped_two = [&](uint32_t s0, uint32_t s1, float& y0, float& y1) {
+    // cap tanh y = cap - 2 cap / (e^(2 y) + 1), within 2^-21 of the cap: a score's error is an absolute one.  Two scores with one
+    // reciprocal (e^(2 y) up to 2^60, where the cap is reached).
+    auto capped_two = [&](uint32_t& s0, uint32_t& s1) {
       const float z0 = exp2_of(least_of(__uint_as_float(s0) * cap_in, 60.0f)) + 1.0f, z1 = exp2_of(least_of(__uint_as_float(s1) * cap_in, 60.0f)) + 1.0f;
       const float f = -2.0f * cap_out * reciprocal(z0 * z1);
-      y0 = fmaf(f, z1, cap_out);
-      y1 = fmaf(f, z0, cap_out);
+      s0 = __float_as_uint(fmaf(f, z1, cap_out));
+      s1 = __float_as_uint(fmaf(f, z0, cap_out));
     };
     int item0 = 0, tile0 = 0;
     uint32_t s_parity = 0, o_parity = 0;             // (of the slot's S; bit i: of slot i's O)
@@ -608,9 +603,21 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const int my_row = pair ? slot * kSlotRows + r : r;
       const int node = min(quotient(g.row0 + min(my_row, g.rows - 1), a.group), g.n - 1);
       const bool idle = my_row - lane >= g.rows;
-      float m = fixed ? 0.0f : -INFINITY;
+      float m = -INFINITY;
       uint64_t l2 = ptx::f2_pack(0.0f, 0.0f);
       bool first_step = true;
+      auto rescale = [&](float f) {                  // O *= f (it is complete up to the tile before: its MMAs came before those of S)
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+          uint32_t o[16];
+          ptx::tmem_ld_16raw(col_o + 128 * slot + 16 * i, o);
+          ptx::tmem_ld_wait();
+          ptx::tmem_regs_ready(o);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+          ptx::tmem_st16(col_o + 128 * slot + 16 * i, o);
+        }
+      };
       for (int k = pair ? 0 : slot; k < n_tiles; k += pair ? 1 : 2) {
         const int T0 = (g.t0 + k) * kTile, info = (tile0 + k) % kInfos;
         wait(&sy.info_full[info], (tile0 + k) / kInfos & 1);
@@ -661,9 +668,23 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         // (A warp without rows leaves its lanes of P as they are: they come into no other row.)
         bool done = idle;
         constexpr int kN = 32;                       // scores at once
+        auto greatest = [](const uint32_t (&x)[kN]) {
+          float t[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) t[j] = fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 4]));
+#pragma unroll
+          for (int j = 8; j < kN; j += 8)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) t[y] = ptx::fmax3(t[y], __uint_as_float(x[j + y]), __uint_as_float(x[j + y + 4]));
+          return fmaxf(ptx::fmax3(t[0], t[1], t[2]), t[3]);
+        };
         if (idle) {
           // (nothing)
-        } else if (kCap && fixed) {
+        } else if constexpr (kCap) {
+          // 32 scores at once, each with the reference as it is by then: capped ones cost too much to be made twice (37 ragged sequences
+          // 73 us; 81 with all 128 in registers as below).  References are whole, so that the weights of the tile that are there
+          // already move with one exactly (down to the type's least).  With 0 for a reference, which bf16 has the range for up to a
+          // cap of 69, it is 69 us, but values of 2^29 overflow next to scores at that cap.
           const uint32_t least = edge ? 0u : Half16<T>::kLeast;
 #pragma unroll 1
           for (int i = 0; i < 4; ++i) {
@@ -678,23 +699,55 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
                 if (!(see >> j & 1u)) x[j] = 0u;
             }
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              float e0, e1;
-              capped_two(x[j], x[j + 1], e0, e1);
-              e0 = exp2_of(e0);
-              e1 = exp2_of(e1);
-              if (edge) {
-                e0 = see >> j & 1u ? e0 : 0.0f;
-                e1 = see >> (j + 1) & 1u ? e1 : 0.0f;
-              }
-              l2 = ptx::f2_add(l2, ptx::f2_pack(e0, e1));
-              w[j / 2] = Half16<T>::weights(e0, e1, least);
+            for (int j = 0; j < 32; j += 2) capped_two(x[j], x[j + 1]);
+            if (edge) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (!(see >> j & 1u)) x[j] = 0xFF800000u;
             }
+            const float top = greatest(x);
+            uint64_t sum;
+#pragma unroll 1
+            for (;;) {                               // (twice where a score is far past the reference)
+              const float base = m == -INFINITY ? 0.0f : Half16<T>::kShift - m;
+              const uint64_t base2 = ptx::f2_pack(base, base);
+              sum = l2;
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                float e0, e1;
+                ptx::f2_unpack(ptx::f2_add(ptx::f2_pack(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), base2), e0, e1);
+                e0 = exp2_of(e0);
+                e1 = exp2_of(e1);
+                sum = ptx::f2_add(sum, ptx::f2_pack(e0, e1));
+                w[j / 2] = Half16<T>::weights(e0, e1, least);
+              }
+              const bool need = top > m + Half16<T>::kLag;
+              if (!__any_sync(0xffffffffu, need)) break;
+              const float next = need ? floorf(top) : m, f = need ? exp2_of(m - next) : 1.0f;
+              if (!first_step) rescale(f);
+              ptx::tmem_wait_st();
+#pragma unroll 1
+              for (int e = 0; e < i; ++e) {
+                ptx::tmem_ld_16raw(col_s + 16 * e, w);
+                ptx::tmem_ld_wait();
+                ptx::tmem_regs_ready(w);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                  const float2 two = widen(T(), w[j]);
+                  w[j] = Half16<T>::weights(two.x * f, two.y * f, least);
+                }
+                ptx::tmem_st16(col_s + 16 * e, w);
+              }
+              l2 = ptx::f2_mul(l2, ptx::f2_pack(f, f));
+              m = next;
+            }
+            l2 = sum;
             ptx::tmem_st16(col_s + 16 * i, w);
           }
           ptx::tmem_wait_st();
+          first_step = false;
           done = true;
-        } else if (!kCap && !first_step && !edge && !in_place) {
+        } else if (!first_step && !edge && !in_place) {
           uint32_t w[4][16];
           float top = -INFINITY;
           const float base = m == -INFINITY ? 0.0f : Half16<T>::kShift - m;
@@ -706,14 +759,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             ptx::tmem_ld_32raw(col_s + kN * i, x);
             ptx::tmem_ld_wait();
             ptx::tmem_regs_ready(x);
-            float t[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) t[j] = fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 4]));
-#pragma unroll
-            for (int j = 8; j < kN; j += 8)
-#pragma unroll
-              for (int y = 0; y < 4; ++y) t[y] = ptx::fmax3(t[y], __uint_as_float(x[j + y]), __uint_as_float(x[j + y + 4]));
-            top = ptx::fmax3(ptx::fmax3(top, t[0], t[1]), t[2], t[3]);
+            top = fmaxf(top, greatest(x));
 #pragma unroll
             for (int j = 0; j < kN; j += 2) {
               float e0, e1;
@@ -732,7 +778,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             done = true;
           }
         }
-        if (!done) {
+        if (!kCap && !done) {
           float top = -INFINITY;
 #pragma unroll 1
           for (int i = 0; i < kTile / kN; ++i) {
@@ -740,10 +786,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             ptx::tmem_ld_32raw(col_s + kN * i, x);
             ptx::tmem_ld_wait();
             ptx::tmem_regs_ready(x);
-            if constexpr (kCap) {
-#pragma unroll
-              for (int j = 0; j < kN; ++j) x[j] = capped(x[j]);
-            } else if (in_place) {
+            if (in_place) {
 #pragma unroll
               for (int j = 0; j < kN; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * cap_in);
             }
@@ -757,32 +800,14 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             if (edge || in_place) {
               ptx::tmem_st32(col_s + kN * i, x);
             }
-            float t[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) t[j] = fmaxf(__uint_as_float(x[j]), __uint_as_float(x[j + 4]));
-#pragma unroll
-            for (int j = 8; j < kN; j += 8)
-#pragma unroll
-              for (int y = 0; y < 4; ++y) t[y] = ptx::fmax3(t[y], __uint_as_float(x[j + y]), __uint_as_float(x[j + y + 4]));
-            top = ptx::fmax3(ptx::fmax3(top, t[0], t[1]), t[2], t[3]);
+            top = fmaxf(top, greatest(x));
           }
           ptx::tmem_wait_st();
           top *= c;
           const bool need = top > m + Half16<T>::kLag;
           if (__any_sync(0xffffffffu, need)) {
             const float f = need ? exp2_of(m - top) : 1.0f;
-            if (!first_step) {                       // (O is complete up to the tile before: its MMAs came before those of S)
-#pragma unroll 1
-              for (int i = 0; i < 8; ++i) {
-                uint32_t o[16];
-                ptx::tmem_ld_16raw(col_o + 128 * slot + 16 * i, o);
-                ptx::tmem_ld_wait();
-                ptx::tmem_regs_ready(o);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                ptx::tmem_st16(col_o + 128 * slot + 16 * i, o);
-              }
-            }
+            if (!first_step) rescale(f);
             l2 = ptx::f2_mul(l2, ptx::f2_pack(f, f));
             if (need) m = top;
           }

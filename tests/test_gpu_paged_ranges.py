@@ -1,0 +1,69 @@
+"""Attention of drafted trees and attention weights where numbers are large, small or many: caps of any size, values and scores at
+the ends of their range, long f16 contexts, free slots of a batch.  On the GPU against the definitions in 64 bits.
+
+Tolerances are those of test_gpu_paged_tokens, with its SCORE for what a score errs by: in these tests scores that come out of
+the tensor cores are under 8 before the cap (asserted), 8 * 8 * 2^-23 = 7.6e-6 of truncation, and a capped one errs by
+2^-21 of the cap up to 64 (3.1e-5), or by 4e-7 of itself (3.2e-6) past that: 3.9e-5 at most.  Where keys and queries have one
+value that is not 0, products are exact, and only the cap's part is left."""
+import math
+
+import numpy as np
+import pytest
+import torch
+from test_gpu_paged_tokens import DEV, SCORE, Drafts, Pool
+
+from paper_2608_14191_gb300 import paged
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _built(aatc):
+    return aatc
+
+
+# ---------------------------------------------------------------- caps
+def one_product(pool, d, keys):
+    """Keys and queries whose only value is the first one: with scale 1 the score of a token is its key's."""
+    d.q.zero_()
+    d.q[..., 0] = 1.0
+    for r, x in enumerate(keys):
+        pool.k[r].zero_()
+        pool.k[r][:, 0, 0] = x
+        pool.put(r)
+
+
+def chain(pool, d, r, s):
+    """out, lse and sum p |v| of a chain's queries with scores s [token] in 64 bits, one kv-head."""
+    n, c = pool.lens[r], d.counts[r]
+    sees = torch.arange(n, device=DEV) <= n - c + torch.arange(c, device=DEV)[:, None]
+    s = torch.where(sees, s.double(), -math.inf)
+    lse = torch.logsumexp(s, 1)
+    p, v = torch.exp(s - lse[:, None]), pool.v[r][:, 0].double()
+    return p @ v, lse, p @ v.abs()
+
+
+@pytest.mark.parametrize("cap", [20.0, 50.0, 64.0, 69.0, 80.0])
+@pytest.mark.parametrize("levels,size", [((3.0, 2.5, 2.75), 2.0 ** 100), ((-3.0, -2.5, -2.75), 2.0 ** -100), ((3.0, -3.0, 0.1), 1.0)], ids=str)
+@pytest.mark.parametrize("heads", [4, 150])
+def test_capped_scores_at_the_cap(heads, levels, size, cap):
+    """All scores near the cap or near its negative, with values at the ends of bf16: the weights are of the size that the
+    scores' differences give, so results of the values' size come out."""
+    rng = np.random.default_rng([int(cap), heads, int(levels[0] + 10)])
+    lens, counts = [700, 300, 129], [2, 1, 3]
+    pool = Pool(rng, lens, 1, 16, torch.bfloat16)
+    for r, n in enumerate(lens):
+        pool.v[r].copy_(torch.from_numpy(rng.uniform(0.5, 1.5, (n, 1, 128)) * size).to(DEV))
+    d = Drafts(rng, pool, counts, heads)
+    one_product(pool, d, [torch.from_numpy(rng.choice(levels, n) * cap).to(DEV) for n in lens])
+    lse = torch.empty((6, heads), device=DEV)
+    out = paged.tree_attention(pool.pages, 0, d.q, pool.table, pool.device_lens, d.starts, lse=lse, scale=1.0, cap=cap)
+    u = 2.0 ** -8
+    for r in range(3):
+        x = pool.k[r][:, 0, 0].double()
+        ref, ref_lse, most = chain(pool, d, r, cap * torch.tanh(x / cap))
+        off = (out[d.of(r)].double() - ref[:, None]).abs()
+        bound = 1.01 * u * (most + ref.abs()) + 2 * SCORE * 1.5 * size
+        assert torch.all(off <= bound[:, None]), (r, float((off / bound[:, None]).max()))
+        assert torch.all((lse[d.of(r)] - ref_lse[:, None]).abs() <= SCORE)
+    assert pool.pages.device_error() == 0
