@@ -51,6 +51,31 @@ __device__ __forceinline__ float tanh_of(float x) {
   const float small = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
   return a < 0.25f ? x * small : copysignf(a > 20.0f ? 1.0f : big, x);
 }
+// cap tanh(s / cap) of a score, given y = s / cap too, in the same way, but the series times s itself: for caps so large that y has
+// left the normal numbers it is s.
+constexpr float kSeries = 0.25f;                               // of y, up to which the series holds
+__device__ __forceinline__ float series_of(float s, float y) {
+  const float y2 = y * y;
+  return s * fmaf(y2, fmaf(y2, fmaf(y2, fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+}
+__device__ __forceinline__ float capped_of(float s, float y, float cap) {
+  const float a = fabsf(y), big = cap * (1.0f - __fdividef(2.0f, exp2_of(2.0f * kLog2e * a) + 1.0f));
+  return a < kSeries ? series_of(s, y) : copysignf(a > 20.0f ? cap : big, y);
+}
+// The same of N scores S, unit S and far_in S being s and y: mostly all of a warp's are in the series' range.
+template <int N>
+__device__ __forceinline__ void cap_far(uint32_t (&x)[N], float unit, float far_in, float cap) {
+  float most = 0.0f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) most = fmaxf(most, fabsf(__uint_as_float(x[j])));
+  if (!__any_sync(0xffffffffu, most * fabsf(far_in) >= kSeries)) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = __float_as_uint(series_of(__uint_as_float(x[j]) * unit, __uint_as_float(x[j]) * far_in));
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = __float_as_uint(capped_of(__uint_as_float(x[j]) * unit, __uint_as_float(x[j]) * far_in, cap));
+  }
+}
 
 }  // namespace paged
 }  // namespace aatc

@@ -245,6 +245,13 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t at, uint32_t lead, uint32
          static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
+// Caps up to here come from cap - 2 cap / (e^(2 s / cap) + 1), whose error is 2^-21 of the cap (3.1e-5 at this one), past it from a
+// form whose error is 4e-7 of the score (37 ragged sequences 73 us with the first, 77 with the second; weights of 32 queries over
+// 3 x 32768 tokens 70 and 66).  They are kernels of their own: both in one cost the first 4 %.
+constexpr float kNearCap = 64.0f;
+constexpr int kNone = 0, kNear = 1, kFar = 2;
+int cap_kind(float cap) { return !(cap > 0.0f) ? kNone : cap <= kNearCap ? kNear : kFar; }
+
 // Bits j .. j + 127 of what query i of the sequence sees of its drafted tokens (ones before them, zeros behind).
 __device__ __forceinline__ void seen_bits(const TreeArgs& a, const Segment& s, int i, int j, uint32_t (&vis)[4]) {
 #pragma unroll
@@ -309,7 +316,7 @@ __device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile 
   return false;
 }
 
-template <typename T, bool kCap>
+template <typename T, int kCap>
 __global__ void __launch_bounds__(kTreeThreads, 1)
     aatc_paged_tree_kernel(const TreeArgs a, const __grid_constant__ CUtensorMap map) {
   extern __shared__ __align__(1024) unsigned char smem[];        // queries of the slots, then the ring
@@ -349,7 +356,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 
   if (warp == kLoadWarp) {
     if (lane == 0) desc[2 * blockIdx.x] = make_int4(-1, 0, 0, 0);
-    Begin at = begin_of(a.batch, kTreeUnits, [&](int i, bool tells) { return units_of<kCap>(a, seq_of(a, i, tells)); });
+    Begin at = begin_of(a.batch, kTreeUnits, [&](int i, bool tells) { return units_of<kCap != kNone>(a, seq_of(a, i, tells)); });
     Pos &x = at.x, &off = at.off;
     const Pos x_end = at.x_end;
     int& b = at.b;
@@ -379,8 +386,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     auto set_block = [&]() {
       hi = seen_to(a, s, block);
       tiles = tiles_to(hi);
-      each = weight_of<kCap>(rows_of(a, s, block));
-      gap = gap_of<kCap>(rows_of(a, s, block));
+      each = weight_of<kCap != kNone>(rows_of(a, s, block));
+      gap = gap_of<kCap != kNone>(rows_of(a, s, block));
       units = static_cast<Pos>(tiles) * each + gap;
     };
     int n_blocks = blocks_of(a, s);
@@ -552,8 +559,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     const uint64_t c2 = ptx::f2_pack(c, c);
     const float cap_in = (kCap ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap_out = a.cap * kLog2e;
     constexpr uint32_t kExponent = Half16<T>::kFormat ? 0x7F807F80u : 0x7C007C00u, kOne = Half16<T>::kFormat ? 0x00800080u : 0x04000400u;
-    // cap tanh y = cap - 2 cap / (e^(2 y) + 1), within 2^-21 of the cap: a score's error is an absolute one.  Two scores with one
-    // reciprocal (e^(2 y) up to 2^60, where the cap is reached).
+    const float far_in = kCap ? a.scale / a.cap : 0.0f, unit = a.scale * kLog2e;
+    // Near caps: cap tanh y = cap - 2 cap / (e^(2 y) + 1), two scores with one reciprocal (e^(2 y) up to 2^60, where the cap is reached).
     auto capped_two = [&](uint32_t& s0, uint32_t& s1) {
       const float z0 = exp2_of(least_of(__uint_as_float(s0) * cap_in, 60.0f)) + 1.0f, z1 = exp2_of(least_of(__uint_as_float(s1) * cap_in, 60.0f)) + 1.0f;
       const float f = -2.0f * cap_out * reciprocal(z0 * z1);
@@ -698,8 +705,12 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               for (int j = 0; j < 32; ++j)
                 if (!(see >> j & 1u)) x[j] = 0u;
             }
+            if constexpr (kCap == kNear) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) capped_two(x[j], x[j + 1]);
+              for (int j = 0; j < 32; j += 2) capped_two(x[j], x[j + 1]);
+            } else {
+              cap_far(x, unit, far_in, cap_out);
+            }
             if (edge) {
 #pragma unroll
               for (int j = 0; j < 32; ++j)
@@ -1091,7 +1102,7 @@ struct SumSync {
   int abort;
 };
 
-template <typename T>
+template <typename T, bool kFarCap>
 __global__ void __launch_bounds__(320, 1) aatc_paged_weights_kernel(const TreeArgs a, const __grid_constant__ CUtensorMap map) {
   extern __shared__ __align__(1024) unsigned char smem[];        // queries, then the ring
   __shared__ SumSync sy;
@@ -1276,8 +1287,8 @@ __global__ void __launch_bounds__(320, 1) aatc_paged_weights_kernel(const TreeAr
     // ---- sums: warp w has tokens 32 (w % 4) .. + 31 of tiles w / 4, w / 4 + 2, ...
     const int buf = warp / 4, r = tid % kTile;
     const uint32_t col = tmem + (static_cast<uint32_t>(32 * (warp % 4)) << 16) + kSumRows * buf;
-    const bool cap = a.cap > 0.0f;
-    const float cap_in = cap ? 2.0f * a.unit / a.cap : 0.0f, cap_out = a.cap * kLog2e;
+    const bool cap = kFarCap || a.cap > 0.0f;
+    const float cap_in = cap ? 2.0f * a.unit / a.cap : 0.0f, far_in = cap ? a.unit * kLn2 / a.cap : 0.0f, cap_out = a.cap * kLog2e;
     const uint64_t unit2 = cap ? ptx::f2_pack(1.0f, 1.0f) : ptx::f2_pack(a.unit, a.odd_unit);
     int tile0 = 0;
     uint32_t s_parity = 0;
@@ -1387,7 +1398,9 @@ __global__ void __launch_bounds__(320, 1) aatc_paged_weights_kernel(const TreeAr
               }
               ptx::tmem_ld_wait();
               ptx::tmem_regs_ready(x);
-              if (cap) {
+              if constexpr (kFarCap) {
+                cap_far(x, a.unit, far_in, cap_out);
+              } else if (cap) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                   x[j] = __float_as_uint(fmaf(-2.0f * cap_out, reciprocal(exp2_of(__uint_as_float(x[j]) * cap_in) + 1.0f), cap_out));
@@ -1458,8 +1471,10 @@ static cudaError_t tile_map(CUtensorMap* map, const Pool& p) {
 cudaError_t launch_tree(int dtype, const TreeArgs& a, cudaStream_t st) {
   const int ctas = std::max(1, a.num_sms);
   const bool bf16 = dtype == AATC_BF16;
-  const auto kernel = a.cap > 0.0f ? (bf16 ? aatc_paged_tree_kernel<__nv_bfloat16, true> : aatc_paged_tree_kernel<__half, true>)
-                                   : (bf16 ? aatc_paged_tree_kernel<__nv_bfloat16, false> : aatc_paged_tree_kernel<__half, false>);
+  constexpr decltype(&aatc_paged_tree_kernel<__half, kNone>) kernels[2][3] = {
+      {aatc_paged_tree_kernel<__half, kNone>, aatc_paged_tree_kernel<__half, kNear>, aatc_paged_tree_kernel<__half, kFar>},
+      {aatc_paged_tree_kernel<__nv_bfloat16, kNone>, aatc_paged_tree_kernel<__nv_bfloat16, kNear>, aatc_paged_tree_kernel<__nv_bfloat16, kFar>}};
+  const auto kernel = kernels[bf16][cap_kind(a.cap)];
   CUtensorMap map;
   cudaError_t e = tile_map(&map, a.pool);
   if (e != cudaSuccess) return e;
@@ -1473,7 +1488,9 @@ cudaError_t launch_tree(int dtype, const TreeArgs& a, cudaStream_t st) {
 }
 
 cudaError_t launch_weights(int dtype, const TreeArgs& a, cudaStream_t st) {
-  const auto kernel = dtype == AATC_BF16 ? aatc_paged_weights_kernel<__nv_bfloat16> : aatc_paged_weights_kernel<__half>;
+  const bool far = cap_kind(a.cap) == kFar;
+  const auto kernel = dtype == AATC_BF16 ? (far ? aatc_paged_weights_kernel<__nv_bfloat16, true> : aatc_paged_weights_kernel<__nv_bfloat16, false>)
+                                         : (far ? aatc_paged_weights_kernel<__half, true> : aatc_paged_weights_kernel<__half, false>);
   CUtensorMap map;
   cudaError_t e = tile_map(&map, a.pool);
   if (e != cudaSuccess) return e;

@@ -10,7 +10,7 @@ import math
 import numpy as np
 import pytest
 import torch
-from test_gpu_paged_tokens import DEV, SCORE, Drafts, Pool
+from test_gpu_paged_tokens import DEV, DTYPES, SCORE, Drafts, Pool, check_tree, check_weights, normal, random_tree, scores_of
 
 from paper_2608_14191_gb300 import paged
 
@@ -58,12 +58,49 @@ def test_capped_scores_at_the_cap(heads, levels, size, cap):
     one_product(pool, d, [torch.from_numpy(rng.choice(levels, n) * cap).to(DEV) for n in lens])
     lse = torch.empty((6, heads), device=DEV)
     out = paged.tree_attention(pool.pages, 0, d.q, pool.table, pool.device_lens, d.starts, lse=lse, scale=1.0, cap=cap)
+    w = paged.attention_weights(pool.pages, 0, d.q, pool.table, pool.device_lens, d.starts, lse, torch.zeros((3, 1, 700), device=DEV),
+                                scale=1.0, cap=cap)
     u = 2.0 ** -8
     for r in range(3):
         x = pool.k[r][:, 0, 0].double()
         ref, ref_lse, most = chain(pool, d, r, cap * torch.tanh(x / cap))
+        sees = torch.arange(lens[r], device=DEV) <= lens[r] - counts[r] + torch.arange(counts[r], device=DEV)[:, None]
+        want = torch.where(sees, torch.exp(cap * torch.tanh(x / cap) - lse[d.of(r)].double().T[:, :, None]), 0.0).sum((0, 1))
+        assert torch.all((w[r, 0, :lens[r]].double() - want).abs() <= 6e-5 * want + 1e-30)       # (a sum of 450 rounds less than a score errs)
         off = (out[d.of(r)].double() - ref[:, None]).abs()
         bound = 1.01 * u * (most + ref.abs()) + 2 * SCORE * 1.5 * size
         assert torch.all(off <= bound[:, None]), (r, float((off / bound[:, None]).max()))
         assert torch.all((lse[d.of(r)] - ref_lse[:, None]).abs() <= SCORE)
     assert pool.pages.device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cap,scale", [(30.0, 0.09), (63.9, 0.09), (64.0, -0.09), (64.1, 0.09), (128.0, 0.09), (400.0, 0.09), (1e3, 0.09),
+                                       (1e4, -0.05), (1e6, 0.09), (1e12, 0.09), (1e30, 0.09), (8e37, 0.09)])
+def test_caps_of_any_size(cap, scale, dtype):
+    """Large caps leave scores as they are, to their own precision: trees, chains, weights."""
+    rng = np.random.default_rng([71])
+    lens, counts = [1, 100, 101, 640, 2011], [1, 40, 7, 64, 5]
+    pool = Pool(rng, lens, 2, 16, dtype, scale=0.7)
+    d = Drafts(rng, pool, counts, 6, [random_tree(rng, n) for n in counts])
+    assert max(float((lambda s: s[s > -math.inf].abs().max())(scores_of(pool, d, r, scale=scale))) for r in range(5)) < 8
+    check_tree(pool, d, cap=cap, scale=scale)
+    check_weights(pool, d, 2011, cap=cap, scale=scale)
+    d = Drafts(rng, pool, counts, 6)
+    check_tree(pool, d, cap=cap, scale=scale)
+    check_weights(pool, d, 2011, decay=0.0, cap=cap, scale=scale)
+
+
+@pytest.mark.parametrize("cap", [30.0, 1e3, 1e6])
+def test_caps_as_the_decode_has_them(cap):
+    """The decode's log-sums with a cap are those of one drafted token, and give weights that sum to the heads."""
+    rng = np.random.default_rng(72)
+    pool = Pool(rng, [900, 33, 4001], 2, 16, torch.bfloat16, scale=0.7)
+    q = normal(rng, (3, 8, 128), torch.bfloat16)
+    step, lse = torch.empty((3, 8), device=DEV), torch.empty((3, 8), device=DEV)
+    paged.decode_attention(pool.pages, 0, q, pool.table, pool.device_lens, lse=step, cap=cap)
+    paged.tree_attention(pool.pages, 0, q, pool.table, pool.device_lens, lse=lse, cap=cap)
+    assert torch.all((step - lse).abs() <= 2 * SCORE)
+    w = torch.zeros((3, 2, 4001), device=DEV)
+    paged.attention_weights(pool.pages, 0, q, pool.table, pool.device_lens, None, step, w, cap=cap)
+    assert torch.all((w.double().sum(2) - 4).abs() <= 2e-4 * 4)
