@@ -642,7 +642,9 @@ aatc_status_t aatc_paged_gather(const aatc_pages_t* desc, const void* pages, con
  *   workspace : device, >= aatc_paged_tree_workspace_bytes, contents ignored; it does not depend on lengths or batch
  * A sequence whose starts, length or mask do not fit (descending starts, more queries than tokens or than mask bits)
  * is flagged (bit 3) and has no results.
- * Softmax and sums are fp32; the weights are rounded to the pages' type before they meet the values, and the result is.
+ * Softmax and sums are fp32; the weights are rounded to the pages' type before they meet the values, and the result is.  In f16
+ * a weight counts as at least 2^-31 of the largest one, less in parts of a context with more than 2^17 tokens: what all tokens of such
+ * weights add to a result is under 2^-14 of their values as long as one SM has no more than 2^24 of them (2^-7 for 2^31).
  * Errors: AATC_ERR_INVALID_ARG (also n_tokens * n_q_heads past 2^31 - 1, batch > 65535), AATC_ERR_WORKSPACE, AATC_ERR_CUDA.
  * n_tokens == 0 is a no-op.
  */

@@ -223,8 +223,10 @@ struct Half16<__half> {
   static constexpr uint32_t kFormat = 0;
   // Weights up to 2^8 of the reference times 2^7 are below the largest number; 11 bits are left of one of 2^-21 of it, and the
   // least is 2^-31: a tail of 131072 such tokens is 2^-14 of a result, an eighth of its rounding.  A lag of 5 (2^10) would leave
-  // 2^-34, but rescales more often: 74 us for 66 (16 x 26 queries of 28 heads over 8192 tokens).
+  // 2^-34, but rescales more often: 74 us for 66 (16 x 26 queries of 28 heads over 8192 tokens).  So a part of a segment that has
+  // more tokens has a lag that is as much smaller, down to 1 for 2^24 tokens, where the least is 2^-38.
   static constexpr float kShift = 7.0f, kLag = 8.0f;
+  static constexpr int kLagTiles = 10, kLagMore = 7;       // log2 of the tiles that kLag is for; that it gives up at most
   static constexpr uint32_t kLeast = 0x00010001u;  // 2^-24, twice
   static __device__ __forceinline__ uint32_t weights(float p, float q, uint32_t least) {
     const __half2 h = __hmax2_nan(__floats2half2_rn(p, q), *reinterpret_cast<const __half2*>(&least));
@@ -613,6 +615,12 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       float m = -INFINITY;
       uint64_t l2 = ptx::f2_pack(0.0f, 0.0f);
       bool first_step = true;
+      float shift = Half16<T>::kShift, lag = Half16<T>::kLag;
+      if constexpr (Half16<T>::kFormat == 0) {
+        const int more = min(max(32 - __clz(n_tiles - 1) - Half16<T>::kLagTiles, 0), Half16<T>::kLagMore);
+        shift += more;
+        lag -= more;
+      }
       auto rescale = [&](float f) {                  // O *= f (it is complete up to the tile before: its MMAs came before those of S)
 #pragma unroll 1
         for (int i = 0; i < 8; ++i) {
@@ -720,7 +728,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             uint64_t sum;
 #pragma unroll 1
             for (;;) {                               // (twice where a score is far past the reference)
-              const float base = m == -INFINITY ? 0.0f : Half16<T>::kShift - m;
+              const float base = m == -INFINITY ? 0.0f : shift - m;
               const uint64_t base2 = ptx::f2_pack(base, base);
               sum = l2;
 #pragma unroll
@@ -732,7 +740,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
                 sum = ptx::f2_add(sum, ptx::f2_pack(e0, e1));
                 w[j / 2] = Half16<T>::weights(e0, e1, least);
               }
-              const bool need = top > m + Half16<T>::kLag;
+              const bool need = top > m + lag;
               if (!__any_sync(0xffffffffu, need)) break;
               const float next = need ? floorf(top) : m, f = need ? exp2_of(m - next) : 1.0f;
               if (!first_step) rescale(f);
@@ -761,7 +769,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         } else if (!first_step && !edge && !in_place) {
           uint32_t w[4][16];
           float top = -INFINITY;
-          const float base = m == -INFINITY ? 0.0f : Half16<T>::kShift - m;
+          const float base = m == -INFINITY ? 0.0f : shift - m;
           const uint64_t base2 = ptx::f2_pack(base, base);
           uint64_t sum = l2;
 #pragma unroll
@@ -781,7 +789,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               w[kN * i / 32][kN * i % 32 / 2 + j / 2] = Half16<T>::weights(e0, e1, Half16<T>::kLeast);
             }
           }
-          if (!__any_sync(0xffffffffu, top * c > m + Half16<T>::kLag)) {
+          if (!__any_sync(0xffffffffu, top * c > m + lag)) {
             l2 = sum;
 #pragma unroll
             for (int i = 0; i < 4; ++i) ptx::tmem_st16(col_s + 16 * i, w[i]);
@@ -815,7 +823,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           }
           ptx::tmem_wait_st();
           top *= c;
-          const bool need = top > m + Half16<T>::kLag;
+          const bool need = top > m + lag;
           if (__any_sync(0xffffffffu, need)) {
             const float f = need ? exp2_of(m - top) : 1.0f;
             if (!first_step) rescale(f);
@@ -823,7 +831,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             if (need) m = top;
           }
           first_step = false;
-          const float base = m == -INFINITY ? 0.0f : Half16<T>::kShift - m;
+          const float base = m == -INFINITY ? 0.0f : shift - m;
           const uint64_t base2 = ptx::f2_pack(base, base);
           const uint32_t least = edge ? 0u : Half16<T>::kLeast;     // where all tokens are seen none is 0: times infinity it would be NaN
 #pragma unroll 1
@@ -921,7 +929,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         m = best;
       }
       const bool whole = g.t0 == 0 && g.t1 == g.tiles, begins = g.t0 == 0;
-      const float m_out = m == -INFINITY ? -INFINITY : m - Half16<T>::kShift;
+      const float m_out = m == -INFINITY ? -INFINITY : m - shift;
       const bool in = my_row < g.rows;
       const int R = g.row0 + my_row, query = in ? quotient(R, a.group) : 0, head = g.h * a.group + R - query * a.group;
       const int64_t out_row = static_cast<int64_t>(g.i0 + query) * a.n_q + head;

@@ -10,7 +10,7 @@ import math
 import numpy as np
 import pytest
 import torch
-from test_gpu_paged_tokens import DEV, DTYPES, SCORE, Drafts, Pool, check_tree, check_weights, normal, random_tree, scores_of
+from test_gpu_paged_tokens import DEV, DTYPES, SCORE, Drafts, Pool, check_tree, check_weights, ints, normal, random_tree, scores_of
 
 from paper_2608_14191_gb300 import paged
 
@@ -104,3 +104,29 @@ def test_caps_as_the_decode_has_them(cap):
     w = torch.zeros((3, 2, 4001), device=DEV)
     paged.attention_weights(pool.pages, 0, q, pool.table, pool.device_lens, None, step, w, cap=cap)
     assert torch.all((w.double().sum(2) - 4).abs() <= 2e-4 * 4)
+
+
+# ---------------------------------------------------------------- long f16 contexts
+@pytest.mark.parametrize("heads", [4, 130])
+@pytest.mark.parametrize("at", [3, 700000])
+def test_small_weights_of_a_long_f16_context(at, heads):
+    """2^20 tokens, all of one sequence in one CTA: one of weight 1 and value 0, the others of weight 2^-40 and value 1.  What a weight
+    is raised to or rounded by is 2^-34 of the largest one at that length, 2^-14 of a value for all of them."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    n, P = 1 << 20, 256
+    pages = paged.Pages(1, 2, 1, P, torch.float16, DEV)
+    pages.data.zero_()
+    pages.data[0, :, 0, 0, :, 0] = -40 * math.log(2)
+    pages.data[0, :, 1] = 1.0
+    pages.data[0, 1, :, 0, at % P] = 0.0
+    table = torch.zeros((sms, n // P), dtype=torch.int32, device=DEV)
+    table[:, at // P] = 1
+    q = torch.zeros((sms, heads, 128), dtype=torch.float16, device=DEV)
+    q[..., 0] = 1.0
+    lse = torch.empty((sms, heads), device=DEV)
+    out = paged.tree_attention(pages, 0, q, table, ints([n] * sms), lse=lse, scale=1.0)
+    small = (n - 1) * math.exp(float(pages.data[0, 0, 0, 0, 0, 0]))
+    ref = small / (1 + small)
+    assert (out.double() - ref).abs().max() <= 2.0 ** -14 + 2.0 ** -25 + 2.0 ** -10 * ref
+    assert (lse.double() - math.log1p(small)).abs().max() <= SCORE
+    assert pages.device_error() == 0
