@@ -634,7 +634,8 @@ aatc_status_t aatc_paged_gather(const aatc_pages_t* desc, const void* pages, con
  * a query that sees nothing gives out = 0, lse = -infinity.  What a token that a query does not see holds never comes into its
  * result, also where that is infinite or NaN.
  *   starts    : device int32 [batch + 1], ascending from 0 or more to n_tokens or less, or NULL: batch == n_tokens, one
- *               query of each sequence.  A sequence may have no queries; results of tokens in no sequence are left as they are.
+ *               query of each sequence, which sees nothing where the length is 0 (a free slot of a batch).  A sequence may have no
+ *               queries; results of tokens in no sequence are left as they are.
  *   q         : device [n_tokens][n_q_heads][128]
  *   mask      : device int32 [n_tokens][mask_words], with at least n bits for every sequence, or NULL
  *   out       : device [n_tokens][n_q_heads][128] of the pages' type, contiguous, apart from q

@@ -16,7 +16,8 @@ namespace paged {
 
 namespace {
 
-// Sequence b: its queries i0 .. i0 + n, the last n of its len tokens.
+// Sequence b: its queries i0 .. i0 + n, the last n of its len tokens.  (Without starts a row of length 0 is a free slot: its query is
+// none of a sequence's, and its results say so.)
 struct Seq {
   int i0, n, len;
   __device__ int before() const { return len - n; }
@@ -26,7 +27,7 @@ __device__ __forceinline__ Seq seq_of(const TreeArgs& a, int b, bool tells) {
   const int len = a.lens[b], most = a.pool.max_pages << a.pool.page_shift;
   s.len = min(max(len, 0), most);
   s.i0 = a.starts ? a.starts[b] : b;
-  const int end = a.starts ? a.starts[b + 1] : b + 1;
+  const int end = a.starts ? a.starts[b + 1] : b + (len != 0);
   const bool ok = len == s.len && s.i0 >= 0 && s.i0 <= end && end <= a.n_tokens && end - s.i0 <= len &&
                   (!a.mask || end - s.i0 <= static_cast<int64_t>(a.mask_words) * 32);
   s.n = ok ? end - s.i0 : 0;
@@ -1022,12 +1023,23 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 }
 
 // Joins the pieces of the segment that CTA blockIdx.x of the first launch began and did not end; a warp a row, a lane four dimensions.
+// And writes the results of free slots: a lane looks at a row of the table, its warp writes.
 constexpr int kJoinRows = 8;
 template <typename T>
 __global__ void __launch_bounds__(kJoinRows * 32) aatc_paged_tree_join_kernel(const TreeArgs a, int n_ctas) {
   const int c0 = blockIdx.x, row = blockIdx.y * kJoinRows + threadIdx.x / 32, lane = threadIdx.x % 32;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
+  if (!a.starts && blockIdx.y == 0) {
+    for (int64_t b0 = 32ll * (c0 * kJoinRows + threadIdx.x / 32); b0 < a.batch; b0 += 32ll * kJoinRows * gridDim.x) {
+      for (uint32_t free = __ballot_sync(0xffffffffu, b0 + lane < a.batch && a.lens[b0 + lane] == 0); free; free &= free - 1) {
+        const int64_t first = (b0 + __ffs(free) - 1) * a.n_q;
+        uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + first * D);
+        for (int i = lane; i < a.n_q * (D / 8); i += 32) out[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = lane; a.lse && i < a.n_q; i += 32) a.lse[first + i] = -INFINITY;
+      }
+    }
+  }
   const int4* desc = reinterpret_cast<const int4*>(a.ws + static_cast<size_t>(n_ctas) * 2 * kTreePiece) + 2 * c0;
   const int4 what = __ldcg(desc);                    // last CTA, kv-head, first row, rows
   if (what.x < 0 || row >= what.w) return;

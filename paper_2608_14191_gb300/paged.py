@@ -384,7 +384,7 @@ def tree_attention(pages: Pages, layer: int, q, table, lens, starts=None, mask=N
                    scale: float | None = None, cap: float = 0.0, workspace=None, stream=None):
     """aatc_paged_tree_attention: attention of every sequence's last tokens, whose keys and values are in its pages.
     q [tokens][n_q_heads][128] (the pages' type), sequence b's are tokens starts[b] .. starts[b + 1] (int32 [batch + 1];
-    None: one of each sequence); lens int32 [batch] with them; mask int32 [tokens][words]: which of its sequence's drafted tokens
+    None: one of each sequence, with results of 0 and -infinity where a length is 0); lens int32 [batch] with them; mask int32 [tokens][words]: which of its sequence's drafted tokens
     each one sees (`tree_masks`), None: those up to itself.  -> out [tokens][n_q_heads][128] of the pages' type; lse: fp32
     [tokens][n_q_heads], written; scale, cap: as decode_attention's."""
     where = "aatc_paged_tree_attention"

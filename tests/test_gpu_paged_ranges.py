@@ -130,3 +130,52 @@ def test_small_weights_of_a_long_f16_context(at, heads):
     assert (out.double() - ref).abs().max() <= 2.0 ** -14 + 2.0 ** -25 + 2.0 ** -10 * ref
     assert (lse.double() - math.log1p(small)).abs().max() <= SCORE
     assert pages.device_error() == 0
+
+
+# ---------------------------------------------------------------- free slots
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_free_slots_without_starts(dtype):
+    """A step of one query each in a batch with free slots (length 0): nothing is flagged, their results are 0 and -infinity, as the
+    decode's are, and the others' as those with starts; also in a captured call whose lengths change."""
+    rng = np.random.default_rng(73)
+    for lens in ([0], [5, 0, 700, 0, 1, 0], [0] * 399 + [17]):
+        pool = Pool(rng, lens, 2, 16, dtype, scale=1.2)
+        n = len(lens)
+        q = normal(rng, (n, 6, 128), dtype)
+        some = [r for r in range(n) if lens[r]]
+        ws = pool.pages.tree_workspace(6)
+        out, lse, step = torch.full((n, 6, 128), 7.0, dtype=dtype, device=DEV), torch.full((n, 6), 7.0, device=DEV), torch.empty((n, 6), device=DEV)
+        call = lambda: paged.tree_attention(pool.pages, 0, q, pool.table, pool.device_lens, out=out, lse=lse, workspace=ws)  # noqa: E731
+        call()
+        paged.decode_attention(pool.pages, 0, q, pool.table, pool.device_lens, lse=step)
+        w = torch.ones((n, 2, 701), device=DEV)
+        paged.attention_weights(pool.pages, 0, q, pool.table, pool.device_lens, None, step, w, decay=0.5)
+        assert pool.pages.device_error() == 0
+        free = [r for r in range(n) if not lens[r]]
+        assert torch.all(out[free] == 0) and torch.all(lse[free] == -math.inf) and torch.all(w[free] == 1)
+        assert torch.all((lse[some] - step[some]).abs() <= 2 * SCORE)
+        for r in some:
+            assert torch.all((w[r, :, :lens[r]].double().sum(1) - 3 - 0.5 * lens[r]).abs() <= 2e-4 * 3 + 2.0 ** -22 * lens[r])
+            assert torch.all(w[r, :, lens[r]:] == 1)
+        if some:
+            d = Drafts(rng, pool, [int(x > 0) for x in lens], 6)
+            d.q = q[some].contiguous()
+            got, got_lse = check_tree(pool, d)
+            assert torch.equal(got, out[some]) and torch.equal(got_lse, lse[some])
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        keep = (out.clone(), lse.clone())
+        pool.device_lens.zero_()
+        out.fill_(7.0)
+        g.replay()
+        assert torch.all(out == 0) and torch.all(lse == -math.inf)
+        pool.device_lens.copy_(ints(lens))
+        g.replay()
+        assert torch.equal(out, keep[0]) and torch.equal(lse, keep[1])
+        paged.tree_attention(pool.pages, 0, q, pool.table, pool.device_lens, out=out.fill_(7.0))
+        assert torch.equal(out, keep[0]) and pool.pages.device_error() == 0
+        # a length below 0 is none
+        pool.device_lens.fill_(-1)
+        call()
+        assert pool.pages.device_error(clear=True) == 8
