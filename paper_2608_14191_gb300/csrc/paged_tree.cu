@@ -288,6 +288,13 @@ __device__ __forceinline__ float reciprocal(float x) {
   return y;
 }
 
+// 2^x for a factor on sums that may hold an infinite value: at least the least number above 0, so that the value stays infinite and
+// does not turn into NaN.  (Finite sums lose 2^-126 and more: next to nothing is left of them either way.)
+__device__ __forceinline__ float factor_of(float x) {
+  const float f = exp2_of(x), least = __uint_as_float(1u);
+  return f < least ? least : f;                      // (NaN stays)
+}
+
 // Named barriers: of all softmax threads, of a slot's.
 __device__ __forceinline__ void both_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 __device__ __forceinline__ void slot_sync(int slot) { asm volatile("bar.sync %0, 128;" ::"r"(2 + slot) : "memory"); }
@@ -743,7 +750,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               }
               const bool need = top > m + lag;
               if (!__any_sync(0xffffffffu, need)) break;
-              const float next = need ? floorf(top) : m, f = need ? exp2_of(m - next) : 1.0f;
+              const float next = need ? floorf(top) : m, f = need ? factor_of(m - next) : 1.0f;
               if (!first_step) rescale(f);
               ptx::tmem_wait_st();
 #pragma unroll 1
@@ -826,7 +833,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           top *= c;
           const bool need = top > m + lag;
           if (__any_sync(0xffffffffu, need)) {
-            const float f = need ? exp2_of(m - top) : 1.0f;
+            const float f = need ? factor_of(m - top) : 1.0f;
             if (!first_step) rescale(f);
             l2 = ptx::f2_mul(l2, ptx::f2_pack(f, f));
             if (need) m = top;
@@ -924,8 +931,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         both_sync();
         const float2 of0 = ml[r], of1 = ml[kSlotRows + r];
         const float best = fmaxf(of0.x, of1.x), base = best == -INFINITY ? 0.0f : best;
-        f0 = exp2_of(of0.x - base);
-        f1 = exp2_of(of1.x - base);
+        f0 = of0.y == 0.0f ? 0.0f : factor_of(of0.x - base);     // (a sum of 0: a part of nothing)
+        f1 = of1.y == 0.0f ? 0.0f : factor_of(of1.x - base);
         l = fmaf(of0.y, f0, of1.y * f1);
         m = best;
       }
@@ -1061,7 +1068,7 @@ __global__ void __launch_bounds__(kJoinRows * 32) aatc_paged_tree_join_kernel(co
     float next = top;
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, m[k]);
-    const float base = next == -INFINITY ? 0.0f : next, r = exp2_of(top - base);
+    const float base = next == -INFINITY ? 0.0f : next, r = factor_of(top - base);
     total *= r;
     sum.x *= r;
     sum.y *= r;
@@ -1069,8 +1076,8 @@ __global__ void __launch_bounds__(kJoinRows * 32) aatc_paged_tree_join_kernel(co
     sum.w *= r;
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const float f = exp2_of(m[k] - base);
-      if (f == 0.0f) continue;                       // (a piece of nothing)
+      if (l[k] == 0.0f) continue;                    // (a piece of nothing)
+      const float f = factor_of(m[k] - base);
       total = fmaf(f, l[k], total);
       sum.x = fmaf(f, o[k].x, sum.x);
       sum.y = fmaf(f, o[k].y, sum.y);

@@ -179,3 +179,25 @@ def test_free_slots_without_starts(dtype):
         pool.device_lens.fill_(-1)
         call()
         assert pool.pages.device_error(clear=True) == 8
+
+
+# ---------------------------------------------------------------- infinite values of tokens far below the others
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads", [4, 150])
+@pytest.mark.parametrize("n,low,strong", [(600, 10, 300), (600, 10, 200), (600, 200, 10), (600, 10, 599), (70001, 10, 69000), (70001, 69000, 10)])
+def test_infinite_value_far_below(n, low, strong, heads, dtype):
+    """One infinite value of a weight of 2^-200 comes out, wherever the line is cut and whichever token is met first; the other
+    dimensions are the strong token's."""
+    rng = np.random.default_rng(74)
+    pool = Pool(rng, [n], 1, 16, dtype)
+    d = Drafts(rng, pool, [1], heads)
+    x = torch.full((n,), -200 * math.log(2), device=DEV)
+    x[strong] = 0.0
+    pool.v[0][low, 0, 7], pool.v[0][low, 0, 9] = math.inf, -math.inf
+    one_product(pool, d, [x])
+    lse = torch.empty((1, heads), device=DEV)
+    out = paged.tree_attention(pool.pages, 0, d.q, pool.table, pool.device_lens, d.starts, lse=lse, scale=1.0)
+    assert torch.all(out[..., 7] == math.inf) and torch.all(out[..., 9] == -math.inf)
+    rest = [i for i in range(128) if i not in (7, 9)]
+    assert torch.all((out[0][:, rest].double() - pool.v[0][strong, 0, rest].double()).abs() <= 2.0 ** -7 * 6)
+    assert torch.all(lse.abs() <= SCORE) and pool.pages.device_error() == 0
