@@ -313,7 +313,7 @@ struct TreeSync {
       info_full[kInfos];
   Segment seg[kSegs];
   uint32_t bad[kInfos];             // a tile's groups of eight tokens whose page is none of the pool's
-  uint32_t special[2][2][4];        // [slot][turn]: tokens of a tile with infinities or NaN among their values
+  uint32_t special[2][3][4];        // [slot][turn]: tokens of a tile with infinities or NaN among their values
   uint32_t tmem;
   int abort;
 };
@@ -646,7 +646,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         wait(&sy.info_full[info], (tile0 + k) / kInfos & 1);
         const uint32_t bad = sy.bad[info];
         const bool edge = g.before - T0 < kTile || bad;      // (T0 + kTile may be 2^31)
-        const int turn = (pair ? tile0 + k : (tile0 + k) / 2) & 1;       // (alternates from one edge tile of a slot to the next)
+        // Tiles that are under way together have turns of their own: a slot that begins a tile is done with the one before the last, but
+        // of a pair the other slot, which reads what the first one found, may have come to that one only.
+        const int turn = pair ? (tile0 + k) % 3 : (tile0 + k) / 2 & 1;
         uint32_t vis[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};   // which of the tile's tokens the row sees
         if (edge) {
           seen_bits(a, g, node, T0 - g.before, vis);

@@ -201,3 +201,33 @@ def test_infinite_value_far_below(n, low, strong, heads, dtype):
     rest = [i for i in range(128) if i not in (7, 9)]
     assert torch.all((out[0][:, rest].double() - pool.v[0][strong, 0, rest].double()).abs() <= 2.0 ** -7 * 6)
     assert torch.all(lse.abs() <= SCORE) and pool.pages.device_error() == 0
+
+
+# ---------------------------------------------------------------- pages outside the pool
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads", [4, 150])
+def test_pages_outside_the_pool_in_every_other_tile(heads, dtype):
+    """Every other tile of 128 tokens has a page outside the pool (flagged, its tokens drop out) and an infinite value, which comes
+    out; the same bits in every run."""
+    rng = np.random.default_rng(76)
+    n, P = 3200, 32
+    pool = Pool(rng, [n], 1, P, dtype, scale=1.2)
+    d = Drafts(rng, pool, [1], heads)
+    tiles = np.arange(0, n // 128, 2)
+    pool.v[0][128 * tiles + 5, 0, tiles] = math.inf
+    pool.put(0)
+    pool.table[0, torch.from_numpy(4 * tiles + 1).to(DEV)] = pool.pages.n_pages
+    left = np.array([t for t in range(n) if not (t // P % 4 == 1 and t // 128 % 2 == 0)])
+    s = scores_of(pool, d, 0)[0][:, left]
+    p, v = torch.softmax(s, 1), torch.where(torch.isfinite(pool.v[0]), pool.v[0], 0.0)[left, 0].double()
+    first = None
+    for _ in range(20):
+        out = paged.tree_attention(pool.pages, 0, d.q, pool.table, pool.device_lens, d.starts)[0]
+        assert pool.pages.device_error(clear=True) == 4
+        assert torch.all(out[:, tiles] == math.inf)
+        rest = np.setdiff1d(np.arange(128), tiles)
+        u = torch.finfo(dtype).eps / 2
+        bound = 1.01 * u * (p @ v.abs() + (p @ v).abs()) + 2 * SCORE * 6 + 2.0 ** -25 + n * 2.0 ** -30 * 6
+        assert torch.all(((out.double() - p @ v).abs() <= bound)[:, rest])
+        first = out if first is None else first
+        assert torch.equal(out, first)
