@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const int32_t* row = p.table + static_cast<int64_t>(b) * p.table_stride;
       auto id_of = [&](int tile) {                   // the page of this lane's box
         const int tok = tile * kTile + lane * rows_box;
-        return lane < n_boxes && tok < hi ? __ldg(row + (tok >> shift)) : 0;
+        return lane < n_boxes && tok < hi ? row[tok >> shift] : 0;
       };
       int id = t < t1 ? id_of(t) : 0;
       for (; t < t1; ++t) {
@@ -1231,7 +1231,7 @@ __global__ void __launch_bounds__(320, 1) aatc_paged_weights_kernel(const TreeAr
         const int32_t* row = p.table + static_cast<int64_t>(b) * p.table_stride;
         auto id_of = [&](int tile) {                 // the page of this lane's box
           const int tok = tile * kTile + lane * rows_box;
-          return lane < n_boxes && tok < hi ? __ldg(row + (tok >> shift)) : 0;
+          return lane < n_boxes && tok < hi ? row[tok >> shift] : 0;
         };
         int id = id_of(t0);
         for (int t = t0; t < t1; ++t, ++item) {

@@ -231,3 +231,32 @@ def test_pages_outside_the_pool_in_every_other_tile(heads, dtype):
         assert torch.all(((out.double() - p @ v).abs() <= bound)[:, rest])
         first = out if first is None else first
         assert torch.equal(out, first)
+
+
+# ---------------------------------------------------------------- tables written just before
+def test_tables_written_by_the_call_before():
+    """Tables, lengths and weights that the call before on the stream writes, over and over: every call sees its own."""
+    rng = np.random.default_rng(77)
+    pool = Pool(rng, [2000, 300], 2, 16, torch.bfloat16, scale=1.2)
+    d = Drafts(rng, pool, [3, 5], 8)
+    tables = [pool.table, pool.table.clone()]
+    used = pool.host[0, :125]
+    tables[1][0, :125] = ints(used[rng.permutation(125)])
+    want = []
+    for t in tables:
+        lse = torch.empty((8, 8), device=DEV)
+        out = paged.tree_attention(pool.pages, 0, d.q, t, pool.device_lens, d.starts, lse=lse)
+        w = torch.zeros((2, 2, 2000), device=DEV)
+        paged.attention_weights(pool.pages, 0, d.q, t, pool.device_lens, d.starts, lse, w)
+        want.append((out, lse, w))
+    table, ws, got = torch.empty_like(tables[0]), pool.pages.tree_workspace(8), []
+    for i in range(60):
+        lse, w = torch.empty((8, 8), device=DEV), torch.zeros((2, 2, 2000), device=DEV)
+        table.copy_(tables[i % 2])
+        out = paged.tree_attention(pool.pages, 0, d.q, table, pool.device_lens, d.starts, lse=lse, workspace=ws)
+        table.copy_(tables[i % 2])
+        paged.attention_weights(pool.pages, 0, d.q, table, pool.device_lens, d.starts, lse, w)
+        got.append((out, lse, w))
+    for i, g in enumerate(got):
+        assert all(torch.equal(x, y) for x, y in zip(g, want[i % 2])), i
+    assert pool.pages.device_error() == 0
