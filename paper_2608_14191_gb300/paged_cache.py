@@ -11,6 +11,8 @@ Everything here runs on the current stream.
 """
 from __future__ import annotations
 
+import operator
+
 import numpy as np
 import torch
 
@@ -190,12 +192,16 @@ class PagedSequences:
         self._push(False)
 
     def _check_weights(self, weights):
+        """All that the operators would refuse, of every layer: once the first layer's tokens have moved it is too late."""
         if weights is None:
             return
         if len(weights) != self.pages.n_layers:
             raise ValueError(f"weights of {self.pages.n_layers} layers needed")
-        if any(w.shape[-1] < self._lens.max() for w in weights):
-            raise ValueError("weights have no room for the longest sequence")
+        rows, heads, most = len(self._lens), self.pages.n_kv_heads, max(1, int(self._lens.max()))
+        for i, w in enumerate(weights):
+            if not isinstance(w, torch.Tensor) or w.device != self.pages.device or w.dtype != torch.float32 or w.dim() != 3 or \
+                    tuple(w.shape[:2]) != (rows, heads) or not most <= w.shape[2] < 1 << 31 or not w.is_contiguous():
+                raise ValueError(f"layer {i}'s weights must be a contiguous float32 tensor [{rows}][{heads}][{most} or more] on {self.pages.device}")
 
     def accept(self, drafted: dict, kept: dict, weights=None):
         """Of the last drafted[row] tokens of every row, in every layer, the ones with the numbers kept[row] (ascending, 0 the first
@@ -237,14 +243,17 @@ class PagedSequences:
         if weights is None:
             raise ValueError("weights needed")
         self._check_weights(weights)
+        keep, first, last = (operator.index(x) for x in (keep, first, last))
         if not 0 <= first + last <= keep or min(first, last) < 0:
             raise ValueError("0 <= first + last <= keep required")
         cut = [int(r) for r in np.flatnonzero(self._lens > keep)]
         if not cut:
             return
+        # (one list for all layers: between the moves nothing is allocated that could fail)
+        kept = torch.empty((len(self._lens), self.pages.n_kv_heads, keep), dtype=torch.int32, device=self.pages.device)
         self._own([(row, min(first, keep), keep) for row in cut])
         for layer, w in enumerate(weights):
-            kept = choose_tokens(w, self.lens, keep, first, last)
+            kept = choose_tokens(w, self.lens, keep, first, last, kept=kept)
             keep_tokens(self.pages, layer, self.table, self.lens, kept, weights=w)
         self._shorten({row: keep for row in cut})
 
