@@ -202,6 +202,9 @@ class PagedSequences:
             if not isinstance(w, torch.Tensor) or w.device != self.pages.device or w.dtype != torch.float32 or w.dim() != 3 or \
                     tuple(w.shape[:2]) != (rows, heads) or not most <= w.shape[2] < 1 << 31 or not w.is_contiguous():
                 raise ValueError(f"layer {i}'s weights must be a contiguous float32 tensor [{rows}][{heads}][{most} or more] on {self.pages.device}")
+        spans = sorted((w.data_ptr(), w.nbytes) for w in weights)
+        if any(at + n > after for (at, n), (after, _) in zip(spans, spans[1:])):
+            raise ValueError("layers share weights, which move with every layer's tokens: give each its own")
 
     def accept(self, drafted: dict, kept: dict, weights=None):
         """Of the last drafted[row] tokens of every row, in every layer, the ones with the numbers kept[row] (ascending, 0 the first
@@ -237,7 +240,7 @@ class PagedSequences:
 
     def evict(self, weights, keep: int, first: int = 0, last: int = 0):
         """Every sequence of more than `keep` tokens is cut to that many: in each layer and kv-head the first `first`, the last `last`
-        and those of most weight between (weights: of every layer fp32 [max_seqs][n_kv_heads][width], as
+        and those of most weight between (weights: of every layer its own fp32 [max_seqs][n_kv_heads][width], as
         attention_weights adds them up; they move with their tokens).  Keys keep the positions that they were turned by, so
         `append` needs positions from then on."""
         if weights is None:

@@ -62,3 +62,22 @@ def test_evictions_with_numbers_that_are_not_whole(lists):
         with pytest.raises(TypeError):
             b.s.evict([torch.rand((3, 1, 64))], *numbers)
         assert np.array_equal(b.s._table, before) and b.s.length(fork) == 40
+
+
+@pytest.mark.parametrize("call", ["accept", "evict"])
+def test_layers_that_share_weights_are_refused(lists, call):
+    """Weights of two layers in one tensor, or in tensors that overlap, would be moved twice."""
+    b = lists(20, 3, 64, 8)
+    b.s.pages = b.s.pages.__class__.of(torch.zeros((2, 20, 2, 1, 8, 128), dtype=torch.bfloat16))
+    b.s.add()
+    b.s.grow({0: 40})
+    run = (lambda w: b.s.evict(w, 16, 2, 4)) if call == "evict" else (lambda w: b.s.accept({0: 9}, {0: [1, 5]}, w))
+    room = torch.rand(6 * 64)
+    one, end, apart = room[:192].view(3, 1, 64), room[191:383].view(3, 1, 64), room[192:].view(3, 1, 64)
+    before = room.clone()
+    for weights in ([one, one], [one, end], [end, one], one[None].expand(2, 3, 1, 64)):
+        with pytest.raises(ValueError, match="weights"):
+            run(weights)
+        assert torch.equal(room, before) and b.s.length(0) == 40
+    run([one, apart])
+    assert b.s.length(0) == (16 if call == "evict" else 33)
