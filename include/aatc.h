@@ -659,7 +659,9 @@ aatc_status_t aatc_paged_tree_attention(const aatc_pages_t* desc, const void* pa
 
 /*
  * The weights that tokens got in an attention, for the choice of those that stay: with the queries, scores and masks of
- * aatc_paged_tree_attention and the log-sums that it wrote (or aatc_paged_decode_attention, without starts and mask),
+ * aatc_paged_tree_attention and the log-sums that it wrote (or aatc_paged_decode_attention, without starts and mask, called with the
+ * same scale and cap and without window and slopes: this call knows neither, and would give tokens outside a window exp(s - lse)
+ * too; joined with another set of tokens, `prior`, its log-sums are those of both sets, and weights are shares of both),
  *   weights[b][h][t] = decay weights[b][h][t] + sum over sequence b's queries that see t and the query heads of kv-head h
  *                      of exp(s_t - lse),   0 <= t < lens[b];
  * weights of other tokens are left as they are.  decay == 0: the old weights are not read.  A log-sum of -infinity gives

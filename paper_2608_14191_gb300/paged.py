@@ -419,8 +419,9 @@ def tree_attention(pages: Pages, layer: int, q, table, lens, starts=None, mask=N
 def attention_weights(pages: Pages, layer: int, q, table, lens, starts, lse, weights, mask=None, scale: float | None = None,
                       cap: float = 0.0, decay: float = 1.0, stream=None):
     """aatc_paged_attention_weights: what every token got in the attention of these queries (as tree_attention takes them, with
-    the lse that it wrote; or decode_attention's, with starts None) is added to weights, fp32 [batch][n_kv_heads][width], which
-    are returned; decay: the factor on what was there (0: nothing is read)."""
+    the lse that it wrote; or decode_attention's, with starts None, of a call with the same scale and cap and without window and
+    slopes, which are not known here; with a prior the weights are shares of both sets) is added to weights, fp32
+    [batch][n_kv_heads][width], which are returned; decay: the factor on what was there (0: nothing is read)."""
     where = "aatc_paged_attention_weights"
     _pages(pages, where)
     base = pages.layer(layer, where)

@@ -203,6 +203,23 @@ def test_infinite_value_far_below(n, low, strong, heads, dtype):
     assert torch.all(lse.abs() <= SCORE) and pool.pages.device_error() == 0
 
 
+# ---------------------------------------------------------------- log-sums of two sets of tokens
+def test_weights_by_the_log_sum_of_two_sets():
+    """A decode joined with another set of tokens has the log-sum of both: weights are shares of that."""
+    rng = np.random.default_rng(75)
+    pool = Pool(rng, [300, 41], 2, 16, torch.bfloat16, scale=1.2)
+    d = Drafts(rng, pool, [1, 1], 8)
+    prior = (torch.randn((2, 8, 128), device=DEV), torch.full((2, 8), 6.0, device=DEV))
+    lse = torch.empty((2, 8), device=DEV)
+    paged.decode_attention(pool.pages, 0, d.q, pool.table, pool.device_lens, lse=lse, prior=prior)
+    w = paged.attention_weights(pool.pages, 0, d.q, pool.table, pool.device_lens, None, lse, torch.zeros((2, 2, 300), device=DEV))
+    for r, n in enumerate(pool.lens):
+        s = scores_of(pool, d, r)[0]
+        both = torch.logaddexp(torch.logsumexp(s, 1), torch.tensor(6.0, dtype=torch.float64, device=DEV))
+        want = torch.exp(s - both[:, None]).view(2, 4, n).sum(1)
+        assert torch.all((w[r, :, :n].double() - want).abs() <= (SCORE + 6e-5) * want + 1e-30)
+
+
 # ---------------------------------------------------------------- pages outside the pool
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("heads", [4, 150])
