@@ -678,7 +678,7 @@ aatc_status_t aatc_paged_attention_weights(const aatc_pages_t* desc, const void*
 
 /*
  * The tokens to keep of every sequence and head: of n = lens[b] tokens all where n <= keep, else the first `first`, the last
- * `last` and of those between the ones of most weight, keep in all; of equal weights the earlier token's goes first, and a NaN
+ * `last` and of those between the ones of most weight, keep in all; of equal weights the earlier token is kept, and a NaN
  * counts as more than any number.
  *   weights : device fp32 [batch][n_heads][width];  lens : device int32 [batch], taken as 0 or the width where it is outside
  *   kept    : device int32 [batch][n_heads][keep]: token indexes, ascending, and -1 behind the last one where n < keep

@@ -71,7 +71,7 @@ __device__ __forceinline__ const T* token_at(const Pool& p, int b, int h, int ki
 // TMEM), the softmax with a lazy reference (O is rescaled only when a row's maximum is 2^8 past it), P in 16 bits over the first half
 // of S, O += P V (P from TMEM, V as it lies).  While one slot's MMAs run, the other slot's softmax does.
 //
-// What bounds it (GB300): 64 queries x 32 heads over 131072 tokens x 8 kv-heads take 109 to 120 us, 4.5 TB/s and 1.2 PFLOP/s, where the
+// What bounds it (GB300): 64 queries x 32 heads over 131072 tokens x 8 kv-heads take 109 to 122 us, 4.9 to 4.4 TB/s, where the
 // memory alone needs 79 and the same kernel without MMAs and softmax takes 94 to 100: a pair's tile costs 1.9 us of softmax and MMAs in
 // turn, 1.5 of memory.  26 queries x 28 heads of 16 sequences over 8192 tokens (f16) 66 us; 37 ragged sequences with capped scores 73
 // (61 without the cap's exponential and half a reciprocal a score): a segment's begin and end, some 7 us for queries, first tiles, results;
@@ -91,10 +91,23 @@ constexpr int kSegs = 4;
 constexpr int kSoftmaxThreads = 256;
 constexpr int kMmaWarp = 0, kLoadWarp = 1, kSoftmaxWarp = 4;   // (warps 2, 3 idle: a warp reaches the TMEM lanes of its number modulo 4)
 constexpr int kTreeThreads = 384;
-// What a segment costs beside its tiles, in units of the line.  With a cap a tile of a pair is two units, as the scores bound it (37 ragged
-// sequences, a third of them pairs: 69 us, 75 with one unit and a gap of 3); without one a tile is one unit, as its copies do. Gaps:
-// capped 73.2 us with 4, 70.4 with 5, 71.0 with 8; not capped 69.4 with 3, 61.9 with 5, 60.8 with 6, 61.8 with 7 (16 x 26 queries over
-// 8192 tokens, all of them pairs: 68.1, 66.6, 65.7, 66.5).
+// What a segment costs beside its tiles, in units of the line.  With a cap a tile of a pair is two units, as the scores bound it; without
+// one a tile is one unit, as its copies do.  Measured in us, sequences x drafted tokens over up to so many tokens:
+//   capped, gaps (pairs' ones)       5 (6)    8 (8)    4 (4)    6 (8)   pairs of one unit, 3 (4)
+//   37 x up to 48 over 4001, ragged   73.5     75.9     77.1     73.2     79.5
+//   the same in f16                   74.5     76.3     78.0     73.8     80.5
+//   37 x 48 over 1000, all alike      85.0     84.1     85.0     84.1     80.3
+//   16 x 26 over 8192 (f16)          102.9    103.0    103.3    102.9    102.3
+//   152 x 32 over 64                  74.5     74.9     74.9     74.9     74.4
+//   8 x 200 over 3000                 51.9     51.2     52.9     51.3     51.7
+//   3 x 16 over 20000                 32.8     33.6     33.0     32.5     32.5
+//   not capped, a gap of                 6        8        3        5        7
+//   the first of these                61.1     63.4     70.0     62.4     62.9
+//   16 x 26 over 8192 (f16)           66.2     68.2     68.6     66.8     66.5
+//   8 x 200 over 3000                 41.7     45.0     43.3     42.4     42.3
+//   3 x 16 over 20000                 29.8     30.6     30.4     30.1     30.1
+//   1 x 64 over 131072               113.8    112.9    115.3    113.8    115.0
+// (the other two within 1 %).
 constexpr int kTreeGap = 6, kTreeGapCapped = 5, kTreeGapCappedPair = 6;
 constexpr int kTreeUnits = 2;                    // of a CTA, at least: every part between a segment's first and last has a tile then
 constexpr uint32_t kColS = 0, kColO = 256;       // TMEM: S (and P) of the slots, then O
@@ -1528,7 +1541,7 @@ cudaError_t launch_weights(int dtype, const TreeArgs& a, cudaStream_t st) {
   // The tensor cores cut their sums off, toward 0: sums of 128 products come out low by 1.35 (bf16) or 2.4 (f16) times 2^-24 of
   // their value on average (measured, 1 to 2.5 over scores of several spreads), which a weight would show.  The unit makes up for
   // it.  As one unit rounds by as much, odd columns have another one, so that both are right on average (a unit's rest, multiplied
-  // and added on its own, is mostly less than half a step of the sum, and lost).
+  // and added on its own, is mostly less than half a step of the sum, and lost).  A single column has its unit's 2^-25 of a score.
   const double low = (dtype == AATC_BF16 ? 1.35 : 2.4) / (1 << 24), unit = static_cast<double>(a.scale) * 1.4426950408889634 * (1.0 + low);
   TreeArgs args = a;
   args.unit = static_cast<float>(unit);
